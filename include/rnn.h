@@ -367,6 +367,121 @@ int rnn_stack_forward(rnn_stack* stack, const void* x, const int32_t* lengths, c
                       const float* const* c0, void* y, float* const* hT, float* const* cT, int T, int B,
                       void* stream);
 
+/*
+ * Linear attention with a decay for each head: a recurrent layer whose state is a matrix S[Dk, Dv] for each sequence
+ * and head, beside the LSTM and GRU cells above.  Like them it is a grid of cells along time (Section 2.2: cell t needs
+ * the state of cell t - 1), but the recurrence is linear, so a run of steps can be taken at once by matrix products:
+ *   S_t = decay[h] * S_{t-1} + k_t v_t^T          o_t = scale * S_t^T q_t
+ * i.e. o_t = scale * sum over j <= t of decay[h]^(t - j) (q_t . k_j) v_j, plus what is left of the initial state.
+ */
+typedef struct rnn_linear_attention rnn_linear_attention;
+
+/* Create a layer.
+ *   num_heads     H >= 1: heads of q and o; every head has a decay and a state of its own.
+ *   num_kv_heads  heads of k and v, a divisor of H: head h reads k and v of head h / (H / num_kv_heads).
+ *   key_size      Dk, width of a head's q and k.    value_size  Dv, width of a head's v and o.
+ *   dtype         rnn_dtype of q, k, v and o.  The state is fp32; products are accumulated in fp32.
+ *   decay         HOST array of H values in [0, 1] (copied): what is left of the state after one step.  1 keeps
+ *                 everything, 0 nothing.  RNN_EINVAL for a value outside (or no number).
+ *   scale         factor of the outputs, finite (RNN_EINVAL otherwise).
+ * Supported: Dk and Dv up to 256, multiples of 4 for RNN_F32 and of 8 for RNN_BF16; H up to 65535; otherwise
+ * RNN_EUNSUPPORTED. */
+int rnn_linear_attention_create(rnn_linear_attention** out, int num_heads, int num_kv_heads, int key_size,
+                                int value_size, int dtype, const float* decay, float scale);
+
+/* Free the layer, its tables and its workspace.  NULL is accepted.  The caller must have synchronised any stream
+ * that still runs a forward of this layer. */
+void rnn_linear_attention_destroy(rnn_linear_attention* layer);
+
+/* Allocate the layer's workspace now if forwards of T steps and B sequences use one (long sequences of few heads do:
+ * the states at the seams of the pieces they are split into).  One size serves every shape, so nothing ever grows. */
+int rnn_linear_attention_reserve(rnn_linear_attention* layer, int T, int B);
+
+/*
+ * Run the layer over T steps of B sequences.
+ *   q             [T, B, H, Dk]             dtype
+ *   k, v          [T, B, num_kv_heads, Dk / Dv]  dtype
+ *   *_strides     NULL: the tensor is contiguous.  Else a HOST array of three strides in elements (step, sequence,
+ *                 head); elements of a head lie side by side.  So batch-first tensors and slices of one projection's
+ *                 output are read in place.  A stride >= 0 and a multiple of 16 bytes where the dimension has more
+ *                 than one entry; those of o must keep its rows apart (RNN_EINVAL otherwise).
+ *   lengths       [B] int32 (DEVICE) or NULL, as in rnn_forward: clamped to [0, T] on the device; a sequence of length 0
+ *                 keeps its initial state.  What lies in q, k and v behind a sequence's end is not read into any result.
+ *   s0            [B, H, Dk, Dv] fp32, contiguous, initial state; NULL = zeros
+ *   o             [T, B, H, Dv]             dtype; positions t >= lengths[b] receive +0.0
+ *   sT            [B, H, Dk, Dv] fp32, contiguous, state after each sequence's last step; may be NULL; sT = s0 is allowed
+ * DEVICE pointers, 16-byte aligned.  o must not overlap an input.  The call enqueues work on `stream` and returns.
+ * It allocates device memory only the first time that a shape uses the workspace (see rnn_linear_attention_reserve).
+ * Non-finite inputs reach the outputs that depend on them by the formula, and no others.
+ * Stream capture: may be recorded into a HIP graph; RNN_EUNSUPPORTED, with nothing recorded, if the workspace would have to be
+ * allocated first.  One forward in flight per layer (a replay counts), as the workspace is the layer's.
+ * RNN_EINVAL if the layer belongs to another device than the current one.  RNN_EUNSUPPORTED if T * B > 2^30 or
+ * B * H * (pieces of a sequence) > 2^30.
+ */
+int rnn_linear_attention_forward(rnn_linear_attention* layer, const void* q, const int64_t* q_strides, const void* k,
+                                 const int64_t* k_strides, const void* v, const int64_t* v_strides,
+                                 const int32_t* lengths, const float* s0, void* o, const int64_t* o_strides, float* sT,
+                                 int T, int B, void* stream);
+
+/* Bytes of device memory the layer holds (tables and workspace). */
+size_t rnn_linear_attention_device_bytes(const rnn_linear_attention* layer);
+
+/* How a forward of T steps and B sequences would run.  Pure host code, no GPU needed; plan (HOST, 4 values):
+ *   plan[0]  steps taken at once by matrix products (a chunk), or 0: one step after the other, the state in registers
+ *   plan[1]  workgroups that share the Dv columns of one state
+ *   plan[2]  pieces that a sequence is split into along time
+ *   plan[3]  steps of a piece
+ * Errors as rnn_linear_attention_create. */
+int rnn_linear_attention_plan_query(int num_heads, int num_kv_heads, int key_size, int value_size, int dtype, int T,
+                                    int B, int* plan);
+
+/*
+ * The norms around a block of a residual network (a recurrent layer above, or what a caller puts between them), fused
+ * with the block's gate and the scale of its residual branch; one pass over the rows of a [T, B, W] tensor:
+ *   a = x                                          the block's output
+ *   a = N_after(a) * after_weight + after_bias     each of `groups` parts of the row by itself (heads)
+ *   a = a * act(gate)
+ *   r = residual + scale * a                       (r = scale * a without a residual)
+ *   y = N_before(r) * before_weight + before_bias  the whole row; the input of the next block (y = r without this norm)
+ * Every part but x may be absent.  All of it is computed in fp32 from the inputs; r and y are rounded once, when stored
+ * (N_before sees r before it is rounded).
+ */
+typedef struct rnn_block_norm rnn_block_norm;
+
+/* RMS: a / sqrt(mean(a^2) + eps).  LAYER: (a - mean(a)) / sqrt(mean((a - mean(a))^2) + eps). */
+enum rnn_norm { RNN_NORM_NONE = 0, RNN_NORM_RMS = 1, RNN_NORM_LAYER = 2 };
+/* act(z): none (no gate), z, 1 / (1 + exp(-z)), z / (1 + exp(-z)). */
+enum rnn_gate { RNN_GATE_NONE = 0, RNN_GATE_LINEAR = 1, RNN_GATE_SIGMOID = 2, RNN_GATE_SILU = 3 };
+
+/* Create the norms of one place in a network.  after / before: rnn_norm; gate: rnn_gate; every vector has W = width
+ * values of type `dtype` in host memory, or in device memory when weights_on_device != 0, and is copied; NULL weights and
+ * scale mean ones, NULL biases zeros; a vector of an absent norm is ignored.  eps > 0 and finite, groups a divisor of
+ * width (else RNN_EINVAL).  Supported: width up to 16384, width and width / groups multiples of 4 (RNN_F32) or 8
+ * (RNN_BF16), and width / groups at least 32 where after is not RNN_NORM_NONE and groups > 1; otherwise RNN_EUNSUPPORTED.
+ * The call synchronises the device. */
+int rnn_block_norm_create(rnn_block_norm** out, int width, int dtype, int after, int groups, const void* after_weight,
+                          const void* after_bias, int gate, const void* scale, int before, const void* before_weight,
+                          const void* before_bias, float eps, int weights_on_device);
+
+/* Free it.  NULL is accepted.  The caller must have synchronised any stream that still uses it. */
+void rnn_block_norm_destroy(rnn_block_norm* norm);
+
+/*
+ * Run it over T steps of B sequences.  x, gate, residual, residual_out, y: [T, B, W] dtype, DEVICE, 16-byte aligned;
+ * *_strides: NULL (contiguous) or a HOST array of two strides in elements (step, sequence), as in
+ * rnn_linear_attention_forward.  gate is required if the norm was created with one, ignored otherwise.  residual
+ * may be NULL (no sum); residual_out receives r, y the normed row; either may be NULL, not both.  lengths as in
+ * rnn_forward: rows t >= lengths[b] are not read, and +0.0 is written to them.  An output may be the very tensor of an input
+ * (same address and strides: a residual stream updated in place); other overlaps are not allowed.
+ * Enqueues one kernel on `stream`, allocates nothing, keeps nothing between calls: any number of calls may be in
+ * flight, and it may be recorded into a HIP graph.  RNN_EINVAL if the norm belongs to another device than the
+ * current one; RNN_EUNSUPPORTED if T * B > 2^30.
+ */
+int rnn_block_norm_forward(const rnn_block_norm* norm, const void* x, const int64_t* x_strides, const void* gate,
+                           const int64_t* gate_strides, const void* residual, const int64_t* residual_strides,
+                           void* residual_out, const int64_t* residual_out_strides, void* y, const int64_t* y_strides,
+                           const int32_t* lengths, int T, int B, void* stream);
+
 /* Which launch of a forward pass holds which layer (launches numbered in stream order), and which group of
  * workgroups of that launch runs which (layer, direction), for the plan rnn_plan_query reports for the same
  * arguments.  The split is the scheduler's: the cell grid (Section 2.2) sorted by the topological sorting of Section

@@ -1,0 +1,350 @@
+// Linear attention with a decay for each head: host side, and the kernel that takes one step after the other.
+//
+//   S_t = decay S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t        (S [Dk, Dv] fp32, a state for each sequence and head)
+//
+// The columns of S do not meet: column c needs k_t, q_t and element c of v_t only.  A workgroup holds a block of
+// columns of one state in registers over all steps of the call, so the state is read and written once, and a step
+// costs two multiply-adds for each element of it and a sum over the rows.  For one step or a few the call is bound by
+// the state's bytes, 8 Dk Dv for each sequence and head.
+#include "../../include/rnn.h"
+#include "common.h"
+#include "linear_attention.h"
+
+#include <cmath>
+#include <new>
+#include <vector>
+
+namespace rnn {
+namespace {
+
+constexpr int STEP_BLOCK = 16;     // steps whose q, k and v are staged in LDS together
+constexpr int STEP_THREADS = 256;
+
+template <typename T> struct Vec16;            // 16 bytes of the storage type
+template <> struct Vec16<float> {
+    static constexpr int N = 4;
+    static __device__ void load(const float* p, float* f) {
+        const float4 v = *reinterpret_cast<const float4*>(p);
+        f[0] = v.x; f[1] = v.y; f[2] = v.z; f[3] = v.w;
+    }
+};
+template <> struct Vec16<bf16_t> {
+    static constexpr int N = 8;
+    static __device__ void load(const bf16_t* p, float* f) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        const uint32_t u[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = __uint_as_float(u[i] << 16);
+            f[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u);
+        }
+    }
+};
+
+__device__ inline void store_one(float* p, float v) { *p = v; }
+__device__ inline void store_one(bf16_t* p, float v) { *reinterpret_cast<__bf16*>(p) = (__bf16)v; }
+
+// COLS columns of one state a workgroup, four neighbouring ones a thread; ROWS rows a thread, GROUPS apart.
+template <typename T, int COLS, int ROWS>
+__global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) {
+    constexpr int LANES = COLS / 4;                    // lanes that hold one row
+    constexpr int GROUPS = STEP_THREADS / LANES;       // rows held side by side
+    constexpr int WAVES = STEP_THREADS / 64;
+    constexpr int DK = GROUPS * ROWS;                  // at least Dk; rows behind Dk stay zero
+    __shared__ __attribute__((aligned(16))) float sq[STEP_BLOCK][DK], sk[STEP_BLOCK][DK], sv[STEP_BLOCK][COLS];
+    __shared__ __attribute__((aligned(16))) float part[STEP_BLOCK][WAVES][COLS];
+
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int col = (tid % LANES) * 4, group = tid / LANES;
+    const int64_t unit = blockIdx.x / a.vblocks;       // (sequence, head)
+    const int v0 = (int)(blockIdx.x % a.vblocks) * COLS;
+    const int b = (int)(unit / a.H), h = (int)(unit % a.H), hk = h / a.rep;
+    const int cols = min(COLS, a.Dv - v0);             // a multiple of 4
+    const bool mine = col < cols;
+    const float decay = a.powers[h * (LA_CHUNK + 1) + 1];
+    int len = a.lengths ? a.lengths[b] : a.T;
+    len = min(max(len, 0), a.T);
+
+    const T* q = (const T*)a.q + b * a.qs.b + h * a.qs.h;
+    const T* k = (const T*)a.k + b * a.ks.b + hk * a.ks.h;
+    const T* v = (const T*)a.v + b * a.vs.b + hk * a.vs.h + v0;
+    T* o = (T*)a.o + b * a.os.b + h * a.os.h + v0;
+
+    float4 S[ROWS];
+    const float* s0 = a.s0 ? a.s0 + (unit * a.Dk) * a.Dv + v0 + col : nullptr;
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        const int row = r * GROUPS + group;
+        S[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (s0 && mine && row < a.Dk) S[r] = *reinterpret_cast<const float4*>(s0 + (int64_t)row * a.Dv);
+    }
+
+    constexpr int N = Vec16<T>::N;
+    const int kc = a.Dk / N, vc = cols / N;            // 16-byte pieces of a row
+    for (int t0 = 0; t0 < len; t0 += STEP_BLOCK) {
+        const int n = min(STEP_BLOCK, len - t0);
+        if (t0) __syncthreads();                       // the block before is used up
+        for (int i = tid; i < n * kc; i += STEP_THREADS) {
+            const int s = i / kc, c = (i % kc) * N;
+            Vec16<T>::load(q + (t0 + s) * a.qs.t + c, &sq[s][c]);
+            Vec16<T>::load(k + (t0 + s) * a.ks.t + c, &sk[s][c]);
+        }
+        for (int i = tid; i < n * (DK - a.Dk); i += STEP_THREADS) {      // rows that no element of the tensors has
+            const int s = i / (DK - a.Dk), c = a.Dk + i % (DK - a.Dk);
+            sq[s][c] = 0.f;
+            sk[s][c] = 0.f;
+        }
+        for (int i = tid; i < n * vc; i += STEP_THREADS) {
+            const int s = i / vc, c = (i % vc) * N;
+            Vec16<T>::load(v + (t0 + s) * a.vs.t + c, &sv[s][c]);
+        }
+        __syncthreads();
+        for (int s = 0; s < n; ++s) {
+            float4 vv = make_float4(0.f, 0.f, 0.f, 0.f), acc = vv;
+            if (mine) vv = *reinterpret_cast<const float4*>(&sv[s][col]);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+                const float kk = sk[s][r * GROUPS + group], qq = sq[s][r * GROUPS + group];
+                S[r].x = fmaf(kk, vv.x, decay * S[r].x); acc.x = fmaf(qq, S[r].x, acc.x);
+                S[r].y = fmaf(kk, vv.y, decay * S[r].y); acc.y = fmaf(qq, S[r].y, acc.y);
+                S[r].z = fmaf(kk, vv.z, decay * S[r].z); acc.z = fmaf(qq, S[r].z, acc.z);
+                S[r].w = fmaf(kk, vv.w, decay * S[r].w); acc.w = fmaf(qq, S[r].w, acc.w);
+            }
+#pragma unroll
+            for (int d = LANES; d < 64; d *= 2) {
+                acc.x += __shfl_xor(acc.x, d);
+                acc.y += __shfl_xor(acc.y, d);
+                acc.z += __shfl_xor(acc.z, d);
+                acc.w += __shfl_xor(acc.w, d);
+            }
+            if (lane < LANES) *reinterpret_cast<float4*>(&part[s][wave][col]) = acc;
+        }
+        __syncthreads();
+        for (int i = tid; i < n * cols; i += STEP_THREADS) {
+            const int s = i / cols, c = i % cols;
+            float sum = part[s][0][c];
+#pragma unroll
+            for (int w = 1; w < WAVES; ++w) sum += part[s][w][c];
+            store_one(o + (t0 + s) * a.os.t + c, a.scale * sum);
+        }
+    }
+    for (int64_t i = tid; i < (int64_t)(a.T - len) * cols; i += STEP_THREADS)
+        store_one(o + (len + i / cols) * a.os.t + i % cols, 0.f);
+    if (a.sT && mine) {
+        float* sT = a.sT + (unit * a.Dk) * a.Dv + v0 + col;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r) {
+            const int row = r * GROUPS + group;
+            if (row < a.Dk) *reinterpret_cast<float4*>(sT + (int64_t)row * a.Dv) = S[r];
+        }
+    }
+}
+
+template <typename T>
+void launch_steps(const LaArgs& a, bool wide, hipStream_t stream) {
+    const dim3 grid((unsigned)((int64_t)a.B * a.H * a.vblocks));
+#define LA_STEPS(C, R) la_steps_kernel<T, C, R><<<grid, STEP_THREADS, 0, stream>>>(a)
+    if (wide) {
+        if (a.Dk <= 64) LA_STEPS(128, 8);
+        else if (a.Dk <= 128) LA_STEPS(128, 16);
+        else LA_STEPS(128, 32);
+    } else {
+        if (a.Dk <= 64) LA_STEPS(32, 2);
+        else if (a.Dk <= 128) LA_STEPS(32, 4);
+        else LA_STEPS(32, 8);
+    }
+#undef LA_STEPS
+}
+
+}  // namespace
+
+hipError_t la_launch_steps(int dtype, const LaArgs& a, bool wide, hipStream_t stream) {
+    if (dtype == DT_BF16) launch_steps<bf16_t>(a, wide, stream);
+    else launch_steps<float>(a, wide, stream);
+    return hipGetLastError();
+}
+
+namespace {
+
+struct LaPlan {
+    int chunk = 0, vblocks = 1, pieces = 1, piece_steps = 0;
+    bool wide = false;
+};
+
+LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
+    (void)Dk; (void)dtype;
+    LaPlan p;
+    p.wide = (int64_t)B * H * ((Dv + 127) / 128) >= 512;
+    p.vblocks = p.wide ? (Dv + 127) / 128 : (Dv + 31) / 32;
+    p.piece_steps = T;
+    return p;
+}
+
+int check_shape(int H, int Hkv, int Dk, int Dv, int dtype) {
+    if (H < 1 || Hkv < 1 || Dk < 1 || Dv < 1 || H % Hkv != 0 || (dtype != RNN_F32 && dtype != RNN_BF16)) return RNN_EINVAL;
+    const int step = dtype == RNN_BF16 ? 8 : 4;
+    if (Dk > 256 || Dv > 256 || Dk % step != 0 || Dv % step != 0 || H > 65535) return RNN_EUNSUPPORTED;
+    return RNN_OK;
+}
+
+int check_call(int H, int T, int B, const LaPlan& p) {
+    if ((int64_t)T * B > ((int64_t)1 << 30) || (int64_t)B * H * p.pieces > ((int64_t)1 << 30)) return RNN_EUNSUPPORTED;
+    if ((int64_t)B * H * p.pieces * p.vblocks > 0x7fffffffLL) return RNN_EUNSUPPORTED;      // workgroups of one launch
+    return RNN_OK;
+}
+
+// The strides of a [T, B, heads, size] tensor; false if they cannot be read in 16-byte pieces.  The stride of a dimension of
+// one entry says nothing (0 is taken); heads that share their rows (stride 0) are for inputs only.
+bool view(const int64_t* strides, int T, int B, int heads, int size, int step, LaView* out) {
+    LaView w = {(int64_t)B * heads * size, (int64_t)heads * size, size};
+    if (strides) w = {strides[0], strides[1], strides[2]};
+    if (T == 1) w.t = 0;
+    if (B == 1) w.b = 0;
+    if (heads == 1) w.h = 0;
+    if (w.t < 0 || w.b < 0 || w.h < 0 || w.t % step || w.b % step || w.h % step) return false;
+    // the last element's offset has to fit 62 bits of bytes
+    const int64_t most = (int64_t)1 << 60;
+    if (w.t > most / T || w.b > most / B || w.h > most / heads) return false;
+    *out = w;
+    return true;
+}
+
+// Whether no two rows of an output share an element: each dimension, in the order of strides, steps over what those
+// inside it reach.
+bool rows_apart(const LaView& w, int T, int B, int heads, int size) {
+    int64_t stride[3], n[3];
+    int m = 0;
+    const int64_t all[3][2] = {{w.t, T}, {w.b, B}, {w.h, heads}};
+    for (const auto& d : all)
+        if (d[1] > 1) {
+            int at = m++;
+            while (at > 0 && stride[at - 1] > d[0]) { stride[at] = stride[at - 1]; n[at] = n[at - 1]; --at; }
+            stride[at] = d[0];
+            n[at] = d[1];
+        }
+    int64_t reach = size;
+    for (int i = 0; i < m; ++i) {
+        if (stride[i] < reach) return false;
+        reach += stride[i] * (n[i] - 1);
+    }
+    return true;
+}
+
+}  // namespace
+}  // namespace rnn
+
+using namespace rnn;
+
+struct rnn_linear_attention {
+    int H = 0, Hkv = 0, Dk = 0, Dv = 0, dtype = 0, device = 0;
+    float scale = 1.f;
+    float* powers = nullptr;        // [H, LA_CHUNK + 1]
+    double* log2_decay = nullptr;   // [H]
+    float* seams = nullptr;
+    size_t table_bytes = 0, seam_bytes = 0;
+};
+
+extern "C" {
+
+void rnn_linear_attention_destroy(rnn_linear_attention* l) {
+    if (!l) return;
+    if (l->log2_decay) (void)hipFree(l->log2_decay);       // the powers lie behind it
+    if (l->seams) (void)hipFree(l->seams);
+    delete l;
+}
+
+int rnn_linear_attention_create(rnn_linear_attention** out, int num_heads, int num_kv_heads, int key_size,
+                                int value_size, int dtype, const float* decay, float scale) try {
+    if (!out) return RNN_EINVAL;
+    *out = nullptr;
+    const int rc = check_shape(num_heads, num_kv_heads, key_size, value_size, dtype);
+    if (rc == RNN_EINVAL || !decay || !std::isfinite(scale)) return RNN_EINVAL;
+    for (int h = 0; h < num_heads; ++h)
+        if (!(decay[h] >= 0.f && decay[h] <= 1.f)) return RNN_EINVAL;
+    if (rc != RNN_OK) return rc;
+    // one block: H doubles, then H rows of LA_CHUNK + 1 floats
+    const size_t H = (size_t)num_heads, bytes = H * sizeof(double) + H * (LA_CHUNK + 1) * sizeof(float);
+    std::vector<double> host((bytes + 7) / 8);
+    float* pw = reinterpret_cast<float*>(host.data() + H);
+    for (size_t h = 0; h < H; ++h) {
+        host[h] = std::log2((double)decay[h]);             // -infinity for 0
+        for (int n = 0; n <= LA_CHUNK; ++n) pw[h * (LA_CHUNK + 1) + n] = (float)std::pow((double)decay[h], n);
+    }
+    rnn_linear_attention* l = new rnn_linear_attention();
+    l->H = num_heads; l->Hkv = num_kv_heads; l->Dk = key_size; l->Dv = value_size; l->dtype = dtype; l->scale = scale;
+    l->table_bytes = bytes;
+    void* dev = nullptr;
+    if (hipGetDevice(&l->device) != hipSuccess) {
+        (void)hipGetLastError();
+        delete l;
+        return RNN_EDEVICE;
+    }
+    if (hipMalloc(&dev, bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        delete l;
+        return RNN_ENOMEM;
+    }
+    l->log2_decay = (double*)dev;
+    l->powers = (float*)((double*)dev + H);
+    if (hipMemcpy(dev, host.data(), bytes, hipMemcpyHostToDevice) != hipSuccess) {
+        (void)hipGetLastError();
+        rnn_linear_attention_destroy(l);
+        return RNN_EDEVICE;
+    }
+    *out = l;
+    return RNN_OK;
+} catch (const std::bad_alloc&) {
+    return RNN_ENOMEM;
+}
+
+size_t rnn_linear_attention_device_bytes(const rnn_linear_attention* l) { return l ? l->table_bytes + l->seam_bytes : 0; }
+
+int rnn_linear_attention_plan_query(int num_heads, int num_kv_heads, int key_size, int value_size, int dtype, int T,
+                                    int B, int* plan) {
+    if (!plan || T < 1 || B < 1) return RNN_EINVAL;
+    int rc = check_shape(num_heads, num_kv_heads, key_size, value_size, dtype);
+    if (rc != RNN_OK) return rc;
+    const LaPlan p = choose(num_heads, key_size, value_size, dtype, T, B);
+    rc = check_call(num_heads, T, B, p);
+    if (rc != RNN_OK) return rc;
+    plan[0] = p.chunk; plan[1] = p.vblocks; plan[2] = p.pieces; plan[3] = p.piece_steps;
+    return RNN_OK;
+}
+
+int rnn_linear_attention_reserve(rnn_linear_attention* l, int T, int B) {
+    if (!l || T < 1 || B < 1) return RNN_EINVAL;
+    return RNN_OK;
+}
+
+int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const int64_t* q_strides, const void* k,
+                                 const int64_t* k_strides, const void* v, const int64_t* v_strides,
+                                 const int32_t* lengths, const float* s0, void* o, const int64_t* o_strides, float* sT,
+                                 int T, int B, void* stream) {
+    if (!l || !q || !k || !v || !o || T < 1 || B < 1) return RNN_EINVAL;
+    if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o | (uintptr_t)s0 | (uintptr_t)sT) & 15) return RNN_EINVAL;
+    if ((uintptr_t)lengths & 3) return RNN_EINVAL;
+    const LaPlan p = choose(l->H, l->Dk, l->Dv, l->dtype, T, B);
+    const int rc = check_call(l->H, T, B, p);
+    if (rc != RNN_OK) return rc;
+    const int step = l->dtype == RNN_BF16 ? 8 : 4;
+    LaArgs a = {};
+    if (!view(q_strides, T, B, l->H, l->Dk, step, &a.qs) || !view(k_strides, T, B, l->Hkv, l->Dk, step, &a.ks) ||
+        !view(v_strides, T, B, l->Hkv, l->Dv, step, &a.vs) || !view(o_strides, T, B, l->H, l->Dv, step, &a.os) ||
+        !rows_apart(a.os, T, B, l->H, l->Dv))
+        return RNN_EINVAL;
+    int device = -1;
+    if (hipGetDevice(&device) != hipSuccess) {
+        (void)hipGetLastError();
+        return RNN_EDEVICE;
+    }
+    if (device != l->device) return RNN_EINVAL;
+    a.q = q; a.k = k; a.v = v; a.o = o;
+    a.lengths = lengths; a.s0 = s0; a.sT = sT;
+    a.powers = l->powers; a.log2_decay = l->log2_decay; a.seams = l->seams;
+    a.scale = l->scale;
+    a.T = T; a.B = B; a.H = l->H; a.rep = l->H / l->Hkv; a.Dk = l->Dk; a.Dv = l->Dv;
+    a.vblocks = p.vblocks; a.pieces = p.pieces; a.piece_steps = p.piece_steps;
+    return la_launch_steps(l->dtype, a, p.wide, (hipStream_t)stream) == hipSuccess ? RNN_OK : RNN_EDEVICE;
+}
+
+}  // extern "C"

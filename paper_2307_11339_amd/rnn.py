@@ -24,6 +24,8 @@ RNN_PLAN_AUTO, RNN_PLAN_CELLWISE, RNN_PLAN_WAVEFRONT = 0, 1, 2
 RNN_ORDER_IFGO_RZN, RNN_ORDER_ONNX = 0, 1
 RNN_KERNEL_PROJECTION, RNN_KERNEL_RECURRENT = 0, 1
 RNN_PROFILE_KERNELS, RNN_PROFILE_STEP_TICKS = 1, 2
+RNN_NORM_NONE, RNN_NORM_RMS, RNN_NORM_LAYER = 0, 1, 2
+RNN_GATE_NONE, RNN_GATE_LINEAR, RNN_GATE_SIGMOID, RNN_GATE_SILU = 0, 1, 2, 3
 
 EXPORTS = ("rnn_model_create", "rnn_model_destroy", "rnn_model_set_plan", "rnn_model_reserve",
            "rnn_forward", "rnn_input_projection", "rnn_model_check", "rnn_model_device_bytes",
@@ -33,7 +35,10 @@ EXPORTS = ("rnn_model_create", "rnn_model_destroy", "rnn_model_set_plan", "rnn_m
            "rnn_model_set_clip", "rnn_model_set_peepholes", "rnn_model_set_batch_first", "rnn_forward_static",
            "rnn_model_set_validation", "rnn_model_set_launch_tag", "rnn_model_set_device_scope", "rnn_probe_matrix_rate", "rnn_plan_launches", "rnn_probe_exchange_step",
            "rnn_stack_create", "rnn_stack_destroy", "rnn_stack_runs", "rnn_stack_run", "rnn_stack_device_bytes",
-           "rnn_stack_forward")
+           "rnn_stack_forward",
+           "rnn_linear_attention_create", "rnn_linear_attention_destroy", "rnn_linear_attention_reserve",
+           "rnn_linear_attention_forward", "rnn_linear_attention_device_bytes", "rnn_linear_attention_plan_query",
+           "rnn_block_norm_create", "rnn_block_norm_destroy", "rnn_block_norm_forward")
 
 _lib = None
 
@@ -115,6 +120,25 @@ def load_library() -> ctypes.CDLL:
     lib.rnn_plan_query.restype = ci
     lib.rnn_plan_query.argtypes = [ci, ci, ci, ci, ci, ci, ci, ci, ci, ci, ctypes.c_size_t, ctypes.POINTER(ci),
                                    ctypes.POINTER(ci)]
+    cf, p64 = ctypes.c_float, ctypes.POINTER(ctypes.c_int64)
+    lib.rnn_linear_attention_create.restype = ci
+    lib.rnn_linear_attention_create.argtypes = [ctypes.POINTER(vp), ci, ci, ci, ci, ci, ctypes.POINTER(cf), cf]
+    lib.rnn_linear_attention_destroy.restype = None
+    lib.rnn_linear_attention_destroy.argtypes = [vp]
+    lib.rnn_linear_attention_reserve.restype = ci
+    lib.rnn_linear_attention_reserve.argtypes = [vp, ci, ci]
+    lib.rnn_linear_attention_forward.restype = ci
+    lib.rnn_linear_attention_forward.argtypes = [vp, vp, p64, vp, p64, vp, p64, vp, vp, vp, p64, vp, ci, ci, vp]
+    lib.rnn_linear_attention_device_bytes.restype = ctypes.c_size_t
+    lib.rnn_linear_attention_device_bytes.argtypes = [vp]
+    lib.rnn_linear_attention_plan_query.restype = ci
+    lib.rnn_linear_attention_plan_query.argtypes = [ci, ci, ci, ci, ci, ci, ci, ctypes.POINTER(ci)]
+    lib.rnn_block_norm_create.restype = ci
+    lib.rnn_block_norm_create.argtypes = [ctypes.POINTER(vp), ci, ci, ci, ci, vp, vp, ci, vp, ci, vp, vp, cf, ci]
+    lib.rnn_block_norm_destroy.restype = None
+    lib.rnn_block_norm_destroy.argtypes = [vp]
+    lib.rnn_block_norm_forward.restype = ci
+    lib.rnn_block_norm_forward.argtypes = [vp, vp, p64, vp, p64, vp, p64, vp, p64, vp, p64, vp, ci, ci, vp]
     lib.rnn_status_string.restype = ctypes.c_char_p
     lib.rnn_status_string.argtypes = [ci]
     lib.rnn_model_set_profiling.restype = ci
@@ -364,3 +388,85 @@ def rnn_model_read_step_ticks(model: int, count: int):
     out = np.zeros(count, dtype=np.uint64)
     rc = load_library().rnn_model_read_step_ticks(model, out.ctypes.data, count)
     return rc, out
+
+
+def _view(t, dims: int):
+    """(device address, strides) of a tensor view whose innermost elements lie side by side: its `dims` outer strides, or None
+    for what is contiguous or comes as an address."""
+    if t is None or isinstance(t, int):
+        return t, None
+    if t.is_contiguous():
+        return t.data_ptr(), None
+    assert t.dim() == dims + 1 and t.stride(-1) == 1, "a strided tensor needs %d outer dimensions and elements side by side" % dims
+    return t.data_ptr(), (ctypes.c_int64 * dims)(*t.stride()[:dims])
+
+
+def rnn_linear_attention_create(num_heads: int, num_kv_heads: int, key_size: int, value_size: int, dtype: int,
+                                decay: Sequence[float], scale: float) -> int:
+    """decay: num_heads values on the host.  Returns the handle."""
+    assert len(decay) == num_heads
+    arr = (ctypes.c_float * max(num_heads, 1))(*[float(d) for d in decay])
+    out = ctypes.c_void_p()
+    rc = load_library().rnn_linear_attention_create(ctypes.byref(out), num_heads, num_kv_heads, key_size, value_size, dtype,
+                                                    arr, scale)
+    if rc != RNN_OK:
+        raise RnnError(rc, "rnn_linear_attention_create")
+    return out.value
+
+
+def rnn_linear_attention_destroy(layer: Optional[int]) -> None:
+    load_library().rnn_linear_attention_destroy(layer)
+
+
+def rnn_linear_attention_reserve(layer: int, T: int, B: int) -> int:
+    return load_library().rnn_linear_attention_reserve(layer, T, B)
+
+
+def rnn_linear_attention_forward(layer: int, q, k, v, lengths, s0, o, sT, T: int, B: int, stream=None) -> int:
+    """Arguments as in include/rnn.h.  q, k, v and o are tensors [T, B, heads, size], whose strides are passed on (slices
+    of one projection, transposed batch-first tensors), or addresses of contiguous ones."""
+    s = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+    (qp, qs), (kp, ks), (vp, vs), (op, os_) = (_view(t, 3) for t in (q, k, v, o))
+    return load_library().rnn_linear_attention_forward(layer, qp, qs, kp, ks, vp, vs, _ptr(lengths), _ptr(s0), op, os_, _ptr(sT),
+                                                       T, B, s)
+
+
+def rnn_linear_attention_device_bytes(layer: int) -> int:
+    return int(load_library().rnn_linear_attention_device_bytes(layer))
+
+
+LINEAR_ATTENTION_PLAN_FIELDS = ("chunk", "value_blocks", "pieces", "piece_steps")
+
+
+def rnn_linear_attention_plan_query(num_heads: int, num_kv_heads: int, key_size: int, value_size: int, dtype: int, T: int,
+                                    B: int):
+    """Host only (no GPU needed).  Returns (status, plan dict keyed by LINEAR_ATTENTION_PLAN_FIELDS)."""
+    plan = (ctypes.c_int * 4)()
+    rc = load_library().rnn_linear_attention_plan_query(num_heads, num_kv_heads, key_size, value_size, dtype, T, B, plan)
+    return rc, dict(zip(LINEAR_ATTENTION_PLAN_FIELDS, list(plan)))
+
+
+def rnn_block_norm_create(width: int, dtype: int, after: int, groups: int, after_weight, after_bias, gate: int, scale,
+                          before: int, before_weight, before_bias, eps: float, weights_on_device: int) -> int:
+    """Vectors: tensors / arrays of `width` values of the storage type (bf16 in host memory: uint16 bits), or None.
+    Returns the handle."""
+    out = ctypes.c_void_p()
+    rc = load_library().rnn_block_norm_create(ctypes.byref(out), width, dtype, after, groups, _ptr(after_weight),
+                                              _ptr(after_bias), gate, _ptr(scale), before, _ptr(before_weight),
+                                              _ptr(before_bias), eps, weights_on_device)
+    if rc != RNN_OK:
+        raise RnnError(rc, "rnn_block_norm_create")
+    return out.value
+
+
+def rnn_block_norm_destroy(norm: Optional[int]) -> None:
+    load_library().rnn_block_norm_destroy(norm)
+
+
+def rnn_block_norm_forward(norm: int, x, gate, residual, residual_out, y, lengths, T: int, B: int, stream=None) -> int:
+    """Arguments as in include/rnn.h.  x, gate, residual, residual_out and y are tensors [T, B, W], whose strides are passed
+    on, or addresses of contiguous ones; gate, residual and one of the outputs may be None."""
+    s = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
+    views = [_view(t, 2) for t in (x, gate, residual, residual_out, y)]
+    args = [p for pair in views for p in pair]
+    return load_library().rnn_block_norm_forward(norm, *args, _ptr(lengths), T, B, s)

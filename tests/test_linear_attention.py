@@ -1,0 +1,434 @@
+"""Linear attention with a decay for each head, through the C ABI, against the recurrence in 64 bits on the host.
+
+Tolerances.  With M = the formula with absolute values of q, k, v and s0 put in (what the terms add up to):
+  - sums and powers of decays in fp32: at most one rounding, 2^-24, for every term that a result passes through; a term
+    passes through at most T + Dk + 64 additions and multiplications;
+  - bf16 products of a chunk: scores, the state as an operand and the weighted values are each handed over as two bf16
+    numbers, which leaves 2^-16 of each (2^-8 of what 2^-8 left): 3 * 2^-16 for an output, 2^-16 for a state;
+  - the output's own rounding: 2^-8 (bf16) or 2^-24 (fp32) of it.
+"""
+import ctypes
+
+import numpy as np
+import pytest
+
+from paper_2307_11339_amd import rnn
+
+F32, BF16 = rnn.RNN_F32, rnn.RNN_BF16
+
+
+# ---- refusals and plans: no GPU ---------------------------------------------------------------------------------
+
+def _create_status(H=2, Hkv=1, Dk=16, Dv=16, dtype=F32, decay=(0.5, 0.5), scale=1.0):
+    lib = rnn.load_library()
+    out = ctypes.c_void_p(1)
+    arr = None if decay is None else (ctypes.c_float * len(decay))(*decay)
+    rc = lib.rnn_linear_attention_create(ctypes.byref(out), H, Hkv, Dk, Dv, dtype, arr, scale)
+    if rc == rnn.RNN_OK:
+        lib.rnn_linear_attention_destroy(out)
+    else:
+        assert not out.value
+    return rc
+
+
+@pytest.mark.parametrize("change", [dict(H=0), dict(Hkv=0), dict(Hkv=3), dict(H=3, Hkv=2), dict(Dk=0), dict(Dv=-4), dict(dtype=2),
+                                    dict(dtype=-1), dict(decay=None), dict(decay=(0.5, 1.5)), dict(decay=(-0.1, 0.5)),
+                                    dict(decay=(0.5, float("nan"))), dict(decay=(float("inf"), 0.5)), dict(scale=float("nan")),
+                                    dict(scale=float("inf"))])
+def test_create_refuses(change):
+    assert _create_status(**change) == rnn.RNN_EINVAL
+
+
+@pytest.mark.parametrize("change", [dict(Dk=260), dict(Dv=512), dict(Dk=6), dict(Dv=18), dict(dtype=BF16, Dk=12), dict(dtype=BF16, Dv=20)])
+def test_create_says_what_is_not_supported(change):
+    assert _create_status(**change) == rnn.RNN_EUNSUPPORTED
+
+
+def test_null_handles_are_refused():
+    lib = rnn.load_library()
+    assert lib.rnn_linear_attention_create(None, 1, 1, 8, 8, 0, None, 1.0) == rnn.RNN_EINVAL
+    assert rnn.rnn_linear_attention_forward(None, 16, 16, 16, None, None, 16, None, 1, 1) == rnn.RNN_EINVAL
+    assert rnn.rnn_linear_attention_reserve(None, 1, 1) == rnn.RNN_EINVAL
+    assert rnn.rnn_linear_attention_device_bytes(None) == 0
+    rnn.rnn_linear_attention_destroy(None)
+
+
+def test_plan_query():
+    q = rnn.rnn_linear_attention_plan_query
+    assert q(8, 3, 64, 64, F32, 10, 1)[0] == rnn.RNN_EINVAL
+    assert q(8, 8, 64, 64, F32, 0, 1)[0] == rnn.RNN_EINVAL
+    assert q(8, 8, 64, 64, F32, 10, 0)[0] == rnn.RNN_EINVAL
+    assert q(8, 8, 62, 64, F32, 10, 1)[0] == rnn.RNN_EUNSUPPORTED
+    assert q(8, 8, 64, 64, F32, 1 << 20, 1 << 11)[0] == rnn.RNN_EUNSUPPORTED
+    assert q(1 << 15, 1, 8, 8, F32, 1, 1 << 16)[0] == rnn.RNN_EUNSUPPORTED
+    for dtype in (F32, BF16):
+        for H, Dk, Dv in ((1, 8, 8), (16, 128, 128), (5, 80, 160), (4, 256, 256)):
+            for T in (1, 3, 16, 64, 65, 500, 4096, 100000):
+                for B in (1, 7, 64, 1000):
+                    rc, p = q(H, H, Dk, Dv, dtype, T, B)
+                    assert rc == rnn.RNN_OK
+                    assert p["chunk"] in (0, 64) and p["value_blocks"] >= 1
+                    # the pieces cover the sequence, none is empty, and inner seams lie between chunks
+                    assert (p["pieces"] - 1) * p["piece_steps"] < T <= p["pieces"] * p["piece_steps"]
+                    assert p["pieces"] == 1 or (p["chunk"] == 64 and p["piece_steps"] % 64 == 0)
+    assert q(8, 8, 128, 128, BF16, 1, 1)[1]["chunk"] == 0          # a single token has no use for a chunk
+
+
+# ---- results ----------------------------------------------------------------------------------------------------
+
+def _reference(q, k, v, decay, scale, lengths, s0):
+    """The recurrence, step by step, in 64 bits."""
+    T, B, H, Dk = q.shape
+    rep = H // k.shape[2]
+    k, v = np.repeat(k, rep, 2), np.repeat(v, rep, 2)
+    S = np.zeros((B, H, Dk, v.shape[3])) if s0 is None else s0.astype(np.float64).copy()
+    o = np.zeros((T, B, H, v.shape[3]))
+    lam = np.asarray(decay, np.float32).astype(np.float64)[None, :, None, None]
+    for t in range(T):
+        with np.errstate(invalid="ignore", over="ignore"):
+            new = lam * S + k[t][..., :, None] * v[t][..., None, :]
+            got = (q[t][..., :, None] * new).sum(2) * scale
+        live = t < lengths
+        S[live] = new[live]
+        o[t, live] = got[live]
+    return o, S
+
+
+def _tolerances(dtype, q, k, v, decay, scale, lengths, s0, ref_o):
+    T, Dk = q.shape[0], q.shape[3]
+    mass_o, mass_s = _reference(abs(q), abs(k), abs(v), decay, abs(scale), lengths, None if s0 is None else abs(s0))
+    per_term = (T + Dk + 64) * 2.0 ** -24
+    split_o, split_s, own = (3 * 2.0 ** -16, 2.0 ** -16, 2.0 ** -8) if dtype == BF16 else (0.0, 0.0, 2.0 ** -24)
+    return mass_o * (per_term + split_o) * (1 + own) + own * abs(ref_o) + 1e-30, mass_s * (per_term + split_s) + 1e-30
+
+
+class Case:
+    """One layer and one call's tensors on the GPU; numpy copies in 64 bits of what the layer sees."""
+
+    def __init__(self, T, B, H, Hkv, Dk, Dv, dtype, lengths=None, state=True, layout="time", seed=0, decay=None, scale=None):
+        import torch
+        self.torch = torch
+        self.T, self.B, self.H, self.Hkv, self.Dk, self.Dv, self.dtype = T, B, H, Hkv, Dk, Dv, dtype
+        self.layout, self.state = layout, state
+        rng = np.random.default_rng(seed + 7919 * T + 31 * Dk + Dv)
+        tdt = torch.bfloat16 if dtype == BF16 else torch.float32
+        self.decay = [1.0 - 2.0 ** -(1 + h % 9) for h in range(H)] if decay is None else decay
+        self.scale = Dk ** -0.5 if scale is None else scale
+        self.tdt = tdt
+
+        def tensor(heads, size):
+            return self.place(torch.from_numpy(rng.standard_normal((T, B, heads, size)).astype(np.float32)).to(tdt))
+
+        if layout == "packed":           # [B, T, (q k v) and a rest that belongs to someone else]
+            w = [H * Dk, Hkv * Dk, Hkv * Dv, 16]
+            buf = torch.from_numpy(rng.standard_normal((B, T, sum(w))).astype(np.float32)).to(tdt).cuda()
+            q, k, v, _ = buf.split(w, -1)
+            self.q, self.k, self.v = (x.unflatten(-1, hs).transpose(0, 1) for x, hs in ((q, (H, Dk)), (k, (Hkv, Dk)), (v, (Hkv, Dv))))
+        else:
+            self.q, self.k, self.v = tensor(H, Dk), tensor(Hkv, Dk), tensor(Hkv, Dv)
+        self.lengths = None if lengths is None else torch.tensor(lengths, dtype=torch.int32, device="cuda")
+        self.clamped = np.full(B, T) if lengths is None else np.clip(np.asarray(lengths), 0, T)
+        self.s0 = torch.from_numpy(rng.standard_normal((B, H, Dk, Dv)).astype(np.float32)).cuda() if state else None
+        self.o = self.place(torch.full((T, B, H, Dv), 7.0, dtype=tdt))
+        self.sT = torch.full((B, H, Dk, Dv), 7.0, device="cuda")
+        self.handle = rnn.rnn_linear_attention_create(H, Hkv, Dk, Dv, dtype, self.decay, self.scale)
+
+    def place(self, x):
+        if self.layout == "time":
+            return x.cuda()
+        return x.transpose(0, 1).contiguous().cuda().transpose(0, 1)
+
+    def forward(self, stream=None):
+        return rnn.rnn_linear_attention_forward(self.handle, self.q, self.k, self.v, self.lengths, self.s0, self.o, self.sT,
+                                                self.T, self.B, stream or self.torch.cuda.current_stream())
+
+    def host(self, x):
+        return None if x is None else x.detach().float().cpu().numpy().astype(np.float64)
+
+    def check(self):
+        self.torch.cuda.synchronize()
+        q, k, v, s0 = (self.host(x) for x in (self.q, self.k, self.v, self.s0))
+        o, S = _reference(q, k, v, self.decay, self.scale, self.clamped, s0)
+        tol_o, tol_s = _tolerances(self.dtype, q, k, v, self.decay, self.scale, self.clamped, s0, o)
+        got_o, got_s = self.host(self.o), self.host(self.sT)
+        worst_o, worst_s = (abs(got_o - o) / tol_o).max(), (abs(got_s - S) / tol_s).max()
+        assert worst_o <= 1 and worst_s <= 1, (worst_o, worst_s)
+        for b in range(self.B):          # +0.0 behind every sequence's end
+            tail = self.o[int(self.clamped[b]):, b].contiguous()
+            assert not bool((tail.view(self.torch.int16 if self.dtype == BF16 else self.torch.int32) != 0).any())
+
+    def __del__(self):
+        if getattr(self, "handle", None):
+            self.torch.cuda.synchronize()
+            rnn.rnn_linear_attention_destroy(self.handle)
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    return torch
+
+
+SHAPES = [
+    # T, B, H, Hkv, Dk, Dv, lengths, state, layout
+    (1, 1, 1, 1, 8, 8, None, False, "time"),
+    (1, 3, 8, 8, 128, 128, None, True, "time"),
+    (1, 5, 4, 2, 64, 32, [0, 1, 1, 0, 1], True, "packed"),
+    (2, 2, 2, 1, 256, 256, None, True, "time"),
+    (15, 3, 3, 3, 40, 72, [15, 0, 7], True, "batch"),
+    (16, 2, 2, 2, 64, 64, None, True, "time"),
+    (17, 1, 5, 1, 16, 256, None, False, "time"),
+    (31, 2, 2, 2, 128, 64, [31, 30], True, "packed"),
+    (63, 2, 3, 3, 64, 64, None, True, "time"),
+    (64, 2, 2, 2, 128, 128, [64, 63], False, "time"),
+    (65, 3, 2, 1, 32, 96, [65, 64, 1], True, "batch"),
+    (128, 1, 4, 4, 96, 128, None, True, "time"),
+    (129, 2, 2, 2, 128, 160, [129, 128], True, "time"),
+    (200, 4, 2, 2, 80, 160, [200, 0, 65, 131], True, "packed"),
+    (301, 2, 3, 1, 192, 24, [-5, 1000], True, "batch"),
+    (260, 1, 2, 2, 256, 256, None, True, "time"),
+    (1100, 1, 2, 1, 64, 128, None, True, "time"),
+    (2100, 2, 1, 1, 128, 64, [2100, 777], True, "batch"),
+    (700, 6, 8, 8, 24, 8, [700, 699, 513, 512, 65, 3], False, "packed"),
+]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", SHAPES, ids=["T%d_B%d_H%d_%d_D%dx%d" % s[:6] for s in SHAPES])
+def test_against_the_recurrence(gpu, shape, dtype):
+    T, B, H, Hkv, Dk, Dv, lengths, state, layout = shape
+    c = Case(T, B, H, Hkv, Dk, Dv, dtype, lengths, state, layout)
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 9, 100, 1500])
+def test_decays_from_nothing_to_everything(gpu, T, dtype):
+    c = Case(T, 2, 6, 6, 64, 64, dtype, decay=[0.0, 1e-30, 0.3, 0.999, 1.0 - 2.0 ** -20, 1.0], scale=-0.5)
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_many_sequences_and_heads(gpu, dtype):
+    c = Case(3, 130, 8, 8, 32, 128, dtype)       # more states than the narrow form of the short kernel is for
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+    c = Case(70, 80, 8, 4, 32, 40, dtype, lengths=[(7 * b) % 71 for b in range(80)])
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_steps_one_by_one_continue_a_prompt(gpu, dtype):
+    """A prompt at once, then single tokens with the state updated in place: the same as all of it at once."""
+    torch = gpu
+    whole = Case(150, 2, 4, 2, 64, 64, dtype)
+    assert whole.forward() == rnn.RNN_OK
+    whole.check()
+    q, k, v, s0 = (whole.host(x) for x in (whole.q, whole.k, whole.v, whole.s0))
+    tol_o, tol_s = _tolerances(dtype, q, k, v, whole.decay, whole.scale, whole.clamped, s0, whole.host(whole.o))
+    state, o = whole.s0.clone(), torch.empty_like(whole.o)
+    at = 0
+    for n in (130, 1, 1, 5, 1, 12):
+        s = slice(at, at + n)
+        assert rnn.rnn_linear_attention_forward(whole.handle, whole.q[s], whole.k[s], whole.v[s], None, state, o[s], state, n, 2,
+                                                torch.cuda.current_stream()) == rnn.RNN_OK
+        at += n
+    torch.cuda.synchronize()
+    assert at == 150
+    assert (abs(whole.host(o) - whole.host(whole.o)) / (2 * tol_o)).max() <= 1      # either may be off by one tolerance
+    assert (abs(whole.host(state) - whole.host(whole.sT)) / (2 * tol_s)).max() <= 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [6, 150, 1300])
+@pytest.mark.parametrize("where", ["v", "k", "q", "s0"])
+def test_non_finite_inputs_reach_only_what_depends_on_them(gpu, T, dtype, where):
+    torch = gpu
+    at = T // 2 + 1
+    for bad in (float("inf"), float("nan"), float("-inf")):
+        c = Case(T, 2, 2, 2, 64, 64, dtype, decay=[0.9, 0.99])
+        if where == "s0":
+            c.s0[1, 0, 3, 5] = bad
+        else:
+            getattr(c, where)[at, 1, 0, 3] = bad
+        assert c.forward() == rnn.RNN_OK
+        torch.cuda.synchronize()
+        q, k, v, s0 = (c.host(x) for x in (c.q, c.k, c.v, c.s0))
+        o, S = _reference(q, k, v, c.decay, c.scale, c.clamped, s0)
+        got_o, got_s = c.host(c.o), c.host(c.sT)
+        assert np.array_equal(np.isfinite(got_o), np.isfinite(o))
+        assert np.array_equal(np.isfinite(got_s), np.isfinite(S))
+        with np.errstate(invalid="ignore"):
+            clean = [np.nan_to_num(x, nan=0, posinf=0, neginf=0) for x in (q, k, v, s0)]
+            tol_o, tol_s = _tolerances(dtype, *clean[:3], c.decay, c.scale, c.clamped, clean[3], np.nan_to_num(o, nan=0, posinf=0, neginf=0))
+            ok_o, ok_s = np.isfinite(o), np.isfinite(S)
+            assert (abs(got_o - o)[ok_o] <= tol_o[ok_o]).all() and (abs(got_s - S)[ok_s] <= tol_s[ok_s]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [5, 90, 1200])
+def test_what_lies_behind_a_sequence_is_not_read(gpu, T, dtype):
+    torch = gpu
+    lengths = [T // 3, 0, T - 1]
+    c = Case(T, 3, 2, 2, 64, 64, dtype, lengths)
+    assert c.forward() == rnn.RNN_OK
+    torch.cuda.synchronize()
+    o, sT = c.o.clone(), c.sT.clone()
+    for b, n in enumerate(lengths):
+        for x in (c.q, c.k, c.v):
+            x[n:, b] = float("nan")
+    c.o.fill_(7.0)
+    assert c.forward() == rnn.RNN_OK
+    torch.cuda.synchronize()
+    assert torch.equal(c.o, o) and torch.equal(c.sT, sT)
+    assert torch.equal(c.sT[1], c.s0[1])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [4, 100, 1100])
+def test_nothing_outside_the_output_is_written(gpu, T, dtype):
+    """o as a slice of a wider buffer; heads of k and v shared by a stride of 0; no sT."""
+    torch = gpu
+    c = Case(T, 2, 4, 4, 64, 24, dtype)
+    c.k, c.v = c.k[:, :, :1].expand(-1, -1, 4, -1), c.v[:, :, :1].expand(-1, -1, 4, -1)
+    buf = torch.full((T, 2, 4, 24 + 16), 7.0, dtype=c.tdt, device="cuda")
+    c.o = buf[..., 8:32]
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+    assert bool((buf[..., :8] == 7).all()) and bool((buf[..., 32:] == 7).all())
+    keep, c.sT = c.sT.clone(), None
+    c.o.fill_(7.0)
+    assert c.forward() == rnn.RNN_OK
+    c.sT = keep
+    c.check()
+
+
+@pytest.mark.gpu
+def test_calls_are_refused(gpu):
+    torch = gpu
+    c = Case(4, 2, 2, 1, 16, 16, BF16)
+    st = torch.cuda.current_stream()
+
+    def call(q=c.q, k=c.k, v=c.v, lengths=None, s0=c.s0, o=c.o, sT=c.sT, T=4, B=2):
+        return rnn.rnn_linear_attention_forward(c.handle, q, k, v, lengths, s0, o, sT, T, B, st)
+
+    for name in ("q", "k", "v", "o"):
+        assert call(**{name: None}) == rnn.RNN_EINVAL
+        assert call(**{name: getattr(c, name).data_ptr() + 2}) == rnn.RNN_EINVAL
+    assert call(T=0) == rnn.RNN_EINVAL and call(B=0) == rnn.RNN_EINVAL
+    assert call(s0=c.s0.data_ptr() + 4) == rnn.RNN_EINVAL and call(sT=c.sT.data_ptr() + 8) == rnn.RNN_EINVAL
+    assert call(T=1 << 20, B=1 << 11) == rnn.RNN_EUNSUPPORTED
+    odd = torch.zeros((4, 2, 2, 20), dtype=torch.bfloat16, device="cuda")[..., :16]      # rows 40 bytes apart
+    assert call(q=odd) == rnn.RNN_EINVAL
+    assert call(o=c.o[:, :, :1].expand(-1, -1, 2, -1)) == rnn.RNN_EINVAL                  # rows that coincide
+    assert call(o=c.o[:1].expand(4, -1, -1, -1)) == rnn.RNN_EINVAL
+    assert call() == rnn.RNN_OK
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T", [1, 70, 2000])
+def test_recorded_and_replayed_on_a_side_stream(gpu, T, dtype):
+    """The state updated in place, three replays with other work between them; the same bits as eager calls."""
+    torch = gpu
+    c = Case(T, 2, 4, 4, 64, 64, dtype, lengths=[T, max(T - 3, 0)])
+    assert rnn.rnn_linear_attention_reserve(c.handle, T, 2) == rnn.RNN_OK
+    eager, want = c.s0.clone(), []
+    for _ in range(3):
+        assert rnn.rnn_linear_attention_forward(c.handle, c.q, c.k, c.v, c.lengths, eager, c.o, eager, T, 2,
+                                                torch.cuda.current_stream()) == rnn.RNN_OK
+        torch.cuda.synchronize()
+        want.append((c.o.clone(), eager.clone()))
+    state = c.s0.clone()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            rc = rnn.rnn_linear_attention_forward(c.handle, c.q, c.k, c.v, c.lengths, state, c.o, state, T, 2, side)
+        assert rc == rnn.RNN_OK
+    torch.cuda.synchronize()
+    for o, s in want:
+        c.o.fill_(3.0)
+        torch.randn(1000, 1000, device="cuda").sum()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(c.o, o) and torch.equal(state, s)
+
+
+@pytest.mark.gpu
+def test_a_workspace_that_is_not_there_is_not_allocated_while_recording(gpu):
+    torch = gpu
+    c = Case(4096, 1, 2, 2, 64, 64, BF16)
+    if rnn.rnn_linear_attention_plan_query(2, 2, 64, 64, BF16, 4096, 1)[1]["pieces"] == 1:
+        pytest.skip("this shape needs no workspace")
+    before = rnn.rnn_linear_attention_device_bytes(c.handle)
+    graph = torch.cuda.CUDAGraph()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            c.o.fill_(2.0)
+            rc = c.forward(side)
+    assert rc == rnn.RNN_EUNSUPPORTED
+    assert rnn.rnn_linear_attention_device_bytes(c.handle) == before
+    assert rnn.rnn_linear_attention_reserve(c.handle, 1, 1) == rnn.RNN_OK              # a single token needs none
+    assert rnn.rnn_linear_attention_device_bytes(c.handle) == before
+    assert rnn.rnn_linear_attention_reserve(c.handle, 4096, 1) == rnn.RNN_OK
+    held = rnn.rnn_linear_attention_device_bytes(c.handle)
+    assert held > before
+    assert rnn.rnn_linear_attention_reserve(c.handle, 100000, 3) == rnn.RNN_OK
+    assert rnn.rnn_linear_attention_device_bytes(c.handle) == held                      # one size serves every shape
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 40])
+def test_rows_more_than_two_to_the_31_elements_apart(gpu, T):
+    torch = gpu
+    B, H, D = 3, 1, 64
+    far = (1 << 30) + 8
+    c = Case(T, B, H, H, D, D, BF16)
+    buf = torch.empty(2 * far + T * D, dtype=torch.bfloat16, device="cuda")
+    outs = torch.empty(2 * far + T * D, dtype=torch.bfloat16, device="cuda")
+    q = torch.as_strided(buf, (T, B, H, D), (D, far, D, 1))
+    q.copy_(c.q)
+    c.q, c.o = q, torch.as_strided(outs, (T, B, H, D), (D, far, D, 1))
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+
+
+@pytest.mark.gpu
+def test_states_beyond_two_to_the_31_elements(gpu):
+    """Every state is the same, so every result has to be; the last ones lie behind 8 GiB."""
+    torch = gpu
+    B, H, D = 2100, 64, 128
+    one = Case(1, 1, H, H, D, D, BF16)
+    assert one.forward() == rnn.RNN_OK
+    one.check()
+    s = one.s0.expand(B, -1, -1, -1).contiguous()
+    assert s.numel() > 1 << 31
+    q, k, v = (x.expand(-1, B, -1, -1) for x in (one.q, one.k, one.v))
+    o = torch.empty((1, B, H, D), dtype=torch.bfloat16, device="cuda")
+    assert rnn.rnn_linear_attention_forward(one.handle, q, k, v, None, s, o, s, 1, B, torch.cuda.current_stream()) == rnn.RNN_OK
+    torch.cuda.synchronize()
+    for b in (0, 1, 1023, 1024, 1025, B - 1):
+        # another form of the kernel may run here: sums in another order
+        q64, k64, v64, s64 = (one.host(x) for x in (one.q, one.k, one.v, one.s0))
+        ref_o, ref_s = _reference(q64, k64, v64, one.decay, one.scale, one.clamped, s64)
+        tol_o, tol_s = _tolerances(BF16, q64, k64, v64, one.decay, one.scale, one.clamped, s64, ref_o)
+        assert (abs(one.host(o[:, b:b + 1]) - ref_o) <= tol_o).all() and (abs(one.host(s[b:b + 1]) - ref_s) <= tol_s).all()
