@@ -15,7 +15,7 @@ SOURCES = ["wavefront_xcd_i.hip", "wavefront_xcd_j.hip", "wavefront_xcd_g.hip", 
            "wavefront_ll.hip", "wavefront_ll_b.hip", "wavefront_ll_c.hip", "wavefront_ll_d.hip", "wavefront_ll_e.hip",
            "wavefront_ll_f.hip", "wavefront_x.hip", "wavefront_x_b.hip", "wavefront.hip", "wavefront_b.hip",
            "rnn_api.hip", "gemm.hip", "cellwise.hip", "schedule.hip", "probe.hip", "rnn_stack.hip",
-           "linear_attention.hip", "block_norm.hip"]   # the slowest first
+           "linear_attention_chunk.hip", "linear_attention_chunk_f32.hip", "linear_attention.hip", "block_norm.hip"]   # the slowest first
 HEADERS = ["common.h", "kernels.h", "wf_traits.h", "linear_attention.h", "wavefront_xcd.hip", "wavefront_ll.hip", "wavefront_x.hip", "wavefront.hip",
            os.path.join("..", "..", "include", "rnn.h"),
            os.path.join("..", "..", "include", "rnn_schedule.h")]

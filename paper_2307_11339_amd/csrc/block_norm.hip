@@ -5,8 +5,9 @@
 // One pass: a row is read once into registers, every mean is taken from there (the variance from the differences to the
 // mean, so nothing cancels), and what is asked for is written once.  Bound by the bytes of its tensors.
 //
-// A thread holds VPT pieces of 16 bytes of a row, the same columns of every row that its workgroup visits.  `lanes` threads
-// hold one group: a power of two, so that a group's sums stay inside a wave or take whole waves.
+// A thread holds VPT pieces of 16 bytes of a row.  `lanes` threads hold one group: a power of two, so that a group's sums stay
+// inside a wave or take whole waves.  The parts that a norm lacks are compiled out (AFTER, GATE, BEFORE): at some twenty
+// vector instructions an element the arithmetic would take as long as the bytes.
 #include "../../include/rnn.h"
 #include "common.h"
 
@@ -18,7 +19,8 @@ namespace rnn {
 namespace {
 
 constexpr int NORM_MAX_WIDTH = 16384;
-constexpr int NORM_MAX_VPT = 8;
+constexpr int NORM_MAX_VPT = 16;
+constexpr int NORM_THREADS = 512;
 
 struct NormLayout {
     int lanes, vpt, slots, rows;   // threads of a group, pieces of a thread, threads of a row, rows of a workgroup
@@ -43,7 +45,8 @@ struct NormArgs {
     const int32_t* lengths;
     int T, B, W, groups;
     int after, before, act;
-    float eps;
+    float eps, per_group, per_row;   // 1 / width of a group, of a row
+    uint32_t divide, shift;          // row / B = row * divide >> shift
     NormLayout lay;
 };
 
@@ -81,39 +84,77 @@ template <> struct Piece<bf16_t> {
     static __device__ inline float silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 };
 
-// Sum over the `lanes` neighbouring threads of a group (a power of two): inside a wave, or over whole waves through LDS.
-__device__ inline float sum_over(float v, int lanes, float* buf) {
-    const int inside = min(lanes, 64);
-    for (int d = 1; d < inside; d *= 2) v += __shfl_xor(v, d);
-    if (lanes <= 64) return v;
-    const int wave = threadIdx.x >> 6, first = wave & -(lanes >> 6);
-    __syncthreads();                       // the sums before are read
-    if ((threadIdx.x & 63) == 0) buf[wave] = v;
-    __syncthreads();
-    float s = 0.f;
-    for (int w = 0; w < (lanes >> 6); ++w) s += buf[first + w];
-    return s;
+template <int CTRL>
+__device__ inline float plus_dpp(float v) {
+    return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
 }
 
-// Sum over all threads of a row: a wave's part if the row is one group inside it, else the workgroup.
-__device__ inline float sum_row(float v, int slots, int waves, float* buf) {
-    if ((slots & (slots - 1)) == 0 && slots <= 64) return sum_over(v, slots, buf);
-    for (int d = 1; d < 64; d *= 2) v += __shfl_xor(v, d);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
-    __syncthreads();
-    float s = 0.f;
-    for (int w = 0; w < waves; ++w) s += buf[w];
-    return s;
+// Sum over `lanes` neighbouring threads of a wave (a power of two, the same for all), the result in each of them.
+__device__ inline float sum_in_wave(float v, int lanes) {
+    if (lanes >= 2) v = plus_dpp<0xB1>(v);             // quad_perm [1, 0, 3, 2]
+    if (lanes >= 4) v = plus_dpp<0x4E>(v);             // quad_perm [2, 3, 0, 1]
+    if (lanes >= 8) v = plus_dpp<0x141>(v);            // row_half_mirror: the other four of eight
+    if (lanes >= 16) v = plus_dpp<0x140>(v);           // row_mirror: the other eight of sixteen
+    if (lanes >= 32) v += __shfl_xor(v, 16);
+    if (lanes >= 64) v += __shfl_xor(v, 32);
+    return v;
 }
+
+// Sums that may cross waves; each uses the buffer that the one before did not, so that one barrier a sum is enough.
+struct Sums {
+    float (*buf)[16];
+    int turn;
+    // over the `lanes` threads of a group: inside a wave, or whole waves
+    __device__ inline float group(float v, int lanes) {
+        v = sum_in_wave(v, min(lanes, 64));
+        if (lanes <= 64) return v;
+        const int n = lanes >> 6, first = (threadIdx.x >> 6) & -n;
+        return across(v, first, n);
+    }
+    // over the threads of a row: inside a wave, or the workgroup
+    __device__ inline float row(float v, int slots, int waves) {
+        if ((slots & (slots - 1)) == 0 && slots <= 64) return sum_in_wave(v, slots);
+        return across(sum_in_wave(v, 64), 0, waves);
+    }
+    __device__ inline float across(float v, int first, int n) {
+        float* b = buf[turn];
+        turn ^= 1;
+        if ((threadIdx.x & 63) == 0) b[threadIdx.x >> 6] = v;
+        __syncthreads();
+        float s = 0.f;
+        for (int w = 0; w < n; ++w) s += b[first + w];
+        return s;
+    }
+};
 
 template <typename T, int VPT>
-__global__ __launch_bounds__(1024) void block_norm_kernel(const NormArgs a) {
+__device__ inline void normalise(float (&f)[VPT][Piece<T>::N], float factor, const T* w, const T* c, const int* col, const bool* has) {
+#pragma unroll
+    for (int i = 0; i < VPT; ++i) {
+        float x[Piece<T>::N];
+#pragma unroll
+        for (int e = 0; e < Piece<T>::N; ++e) f[i][e] *= factor;
+        if (w && has[i]) {
+            Piece<T>::unpack(*reinterpret_cast<const uint4*>(w + col[i]), x);
+#pragma unroll
+            for (int e = 0; e < Piece<T>::N; ++e) f[i][e] *= x[e];
+        }
+        if (c && has[i]) {
+            Piece<T>::unpack(*reinterpret_cast<const uint4*>(c + col[i]), x);
+#pragma unroll
+            for (int e = 0; e < Piece<T>::N; ++e) f[i][e] += x[e];
+        }
+    }
+}
+
+template <typename T, int VPT, bool AFTER, bool GATE, bool BEFORE>
+__global__ __launch_bounds__(NORM_THREADS) void block_norm_kernel(const NormArgs a) {
     constexpr int N = Piece<T>::N;
-    __shared__ float buf[16];
+    __shared__ float buf[2][16];
+    Sums sums = {buf, 0};
     const int waves = blockDim.x >> 6;
-    const int slot = threadIdx.x % a.lay.slots, sub = threadIdx.x / a.lay.slots;
-    const int group = slot / a.lay.lanes, lane = slot % a.lay.lanes;
+    const int slot = threadIdx.x % (unsigned)a.lay.slots, sub = threadIdx.x / (unsigned)a.lay.slots;
+    const int group = slot / (unsigned)a.lay.lanes, lane = slot % (unsigned)a.lay.lanes;
     const int gw = a.W / a.groups;                      // width of a group
     const uint4 zero = make_uint4(0, 0, 0, 0);
 
@@ -126,122 +167,118 @@ __global__ __launch_bounds__(1024) void block_norm_kernel(const NormArgs a) {
         col[i] = has[i] ? group * gw + c : 0;
     }
 
-    const int64_t rows = (int64_t)a.T * a.B;
-    for (int64_t r0 = (int64_t)blockIdx.x * a.lay.rows; r0 < rows; r0 += (int64_t)gridDim.x * a.lay.rows) {
-        const int64_t row = r0 + sub;
+    const uint32_t rows = (uint32_t)a.T * a.B, step = gridDim.x * a.lay.rows;        // at most 2^30 and 2^21
+    for (uint32_t r0 = blockIdx.x * a.lay.rows; r0 < rows; r0 += step) {
+        const uint32_t row = r0 + sub;
         const bool in = sub < a.lay.rows && row < rows;
-        const int t = in ? (int)(row / a.B) : 0, b = in ? (int)(row % a.B) : 0;
-        const bool live = in && (!a.lengths || t < a.lengths[b]);
+        const uint32_t t = in ? (uint32_t)(((uint64_t)row * a.divide) >> a.shift) : 0, b = in ? row - t * a.B : 0;
+        const bool live = in && (!a.lengths || (int)t < a.lengths[b]);
         uint4 px[VPT], pg[VPT], pr[VPT];
+        const T* x = (const T*)a.x + t * a.xs.t + b * a.xs.b;
+        const T* gate = GATE ? (const T*)a.gate + t * a.gs.t + b * a.gs.b : nullptr;
+        const T* residual = a.residual ? (const T*)a.residual + t * a.rs.t + b * a.rs.b : nullptr;
 #pragma unroll
         for (int i = 0; i < VPT; ++i) {
             px[i] = pg[i] = pr[i] = zero;
             if (!live || !has[i]) continue;
-            px[i] = *reinterpret_cast<const uint4*>((const T*)a.x + t * a.xs.t + b * a.xs.b + col[i]);
-            if (a.act) pg[i] = *reinterpret_cast<const uint4*>((const T*)a.gate + t * a.gs.t + b * a.gs.b + col[i]);
-            if (a.residual) pr[i] = *reinterpret_cast<const uint4*>((const T*)a.residual + t * a.rs.t + b * a.rs.b + col[i]);
+            px[i] = *reinterpret_cast<const uint4*>(x + col[i]);
+            if (GATE) pg[i] = *reinterpret_cast<const uint4*>(gate + col[i]);
+            if (a.residual) pr[i] = *reinterpret_cast<const uint4*>(residual + col[i]);
         }
         float f[VPT][N];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) Piece<T>::unpack(px[i], f[i]);
 
-        if (a.after) {
-            float mean = 0.f;
+        if (AFTER) {
+            float s = 0.f;
             if (a.after == RNN_NORM_LAYER) {
-                float s = 0.f;
 #pragma unroll
                 for (int i = 0; i < VPT; ++i)
 #pragma unroll
                     for (int e = 0; e < N; ++e) s += f[i][e];         // pieces behind the group are zero
-                mean = sum_over(s, a.lay.lanes, buf) / gw;
+                const float mean = sums.group(s, a.lay.lanes) * a.per_group;
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) f[i][e] = has[i] ? f[i][e] - mean : 0.f;
+                s = 0.f;
             }
-            float s = 0.f;
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
 #pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    f[i][e] -= mean;
-                    if (has[i]) s = fmaf(f[i][e], f[i][e], s);
-                }
-            const float inv = 1.0f / sqrtf(sum_over(s, a.lay.lanes, buf) / gw + a.eps);
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                float w[N], c[N];
-                Piece<T>::unpack(a.aw ? *reinterpret_cast<const uint4*>((const T*)a.aw + col[i]) : zero, w);
-                Piece<T>::unpack(a.ab ? *reinterpret_cast<const uint4*>((const T*)a.ab + col[i]) : zero, c);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    f[i][e] *= inv;
-                    if (a.aw) f[i][e] *= w[e];
-                    if (a.ab) f[i][e] += c[e];
-                }
-            }
+                for (int e = 0; e < N; ++e) s = fmaf(f[i][e], f[i][e], s);
+            normalise<T, VPT>(f, 1.0f / sqrtf(sums.group(s, a.lay.lanes) * a.per_group + a.eps), (const T*)a.aw, (const T*)a.ab, col, has);
         }
-        if (a.act) {
+        if (GATE) {
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 float z[N];
                 Piece<T>::unpack(pg[i], z);
+                if (a.act == RNN_GATE_SILU) {
 #pragma unroll
-                for (int e = 0; e < N; ++e)
-                    f[i][e] *= a.act == RNN_GATE_LINEAR ? z[e] : a.act == RNN_GATE_SIGMOID ? Piece<T>::sigmoid(z[e]) : Piece<T>::silu(z[e]);
+                    for (int e = 0; e < N; ++e) f[i][e] *= Piece<T>::silu(z[e]);
+                } else if (a.act == RNN_GATE_SIGMOID) {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) f[i][e] *= Piece<T>::sigmoid(z[e]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < N; ++e) f[i][e] *= z[e];
+                }
             }
         }
+        if (a.sc) {
 #pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-            float w[N], c[N];
-            Piece<T>::unpack(a.sc ? *reinterpret_cast<const uint4*>((const T*)a.sc + col[i]) : zero, w);
-            Piece<T>::unpack(pr[i], c);
+            for (int i = 0; i < VPT; ++i)
+                if (has[i]) {
+                    float w[N];
+                    Piece<T>::unpack(*reinterpret_cast<const uint4*>((const T*)a.sc + col[i]), w);
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                if (a.sc) f[i][e] *= w[e];
-                if (a.residual) f[i][e] += c[e];
+                    for (int e = 0; e < N; ++e) f[i][e] *= w[e];
+                }
+        }
+        if (a.residual) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                float c[N];
+                Piece<T>::unpack(pr[i], c);
+#pragma unroll
+                for (int e = 0; e < N; ++e) f[i][e] += c[e];
             }
         }
         if (a.residual_out && in) {
+            T* to = (T*)a.residual_out + t * a.os.t + b * a.os.b;
+#pragma unroll
+            for (int i = 0; i < VPT; ++i)
+                if (has[i]) *reinterpret_cast<uint4*>(to + col[i]) = live ? Piece<T>::pack(f[i]) : zero;
+        }
+        if (!a.y) continue;                                // the same for all threads
+        if (BEFORE) {
+            // pieces behind the group may hold a bias by now
+            float s = 0.f;
+            if (a.before == RNN_NORM_LAYER) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) s += has[i] ? f[i][e] : 0.f;
+                const float mean = sums.row(s, a.lay.slots, waves) * a.per_row;
+#pragma unroll
+                for (int i = 0; i < VPT; ++i)
+#pragma unroll
+                    for (int e = 0; e < N; ++e) f[i][e] -= mean;
+                s = 0.f;
+            }
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
                 if (has[i])
-                    *reinterpret_cast<uint4*>((T*)a.residual_out + t * a.os.t + b * a.os.b + col[i]) = live ? Piece<T>::pack(f[i]) : zero;
-        }
-        if (!a.y) continue;                                // the same for all threads
-        if (a.before) {
-            float mean = 0.f;
-            if (a.before == RNN_NORM_LAYER) {
-                float s = 0.f;
 #pragma unroll
-                for (int i = 0; i < VPT; ++i)
-                    if (has[i])
-#pragma unroll
-                        for (int e = 0; e < N; ++e) s += f[i][e];
-                mean = sum_row(s, a.lay.slots, waves, buf) / a.W;
-            }
-            float s = 0.f;
-#pragma unroll
-            for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    f[i][e] -= mean;
-                    if (has[i]) s = fmaf(f[i][e], f[i][e], s);
-                }
-            const float inv = 1.0f / sqrtf(sum_row(s, a.lay.slots, waves, buf) / a.W + a.eps);
-#pragma unroll
-            for (int i = 0; i < VPT; ++i) {
-                float w[N], c[N];
-                Piece<T>::unpack(a.bw ? *reinterpret_cast<const uint4*>((const T*)a.bw + col[i]) : zero, w);
-                Piece<T>::unpack(a.bb ? *reinterpret_cast<const uint4*>((const T*)a.bb + col[i]) : zero, c);
-#pragma unroll
-                for (int e = 0; e < N; ++e) {
-                    f[i][e] *= inv;
-                    if (a.bw) f[i][e] *= w[e];
-                    if (a.bb) f[i][e] += c[e];
-                }
-            }
+                    for (int e = 0; e < N; ++e) s = fmaf(f[i][e], f[i][e], s);
+            normalise<T, VPT>(f, 1.0f / sqrtf(sums.row(s, a.lay.slots, waves) * a.per_row + a.eps), (const T*)a.bw, (const T*)a.bb, col, has);
         }
         if (in) {
+            T* to = (T*)a.y + t * a.ys.t + b * a.ys.b;
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
-                if (has[i]) *reinterpret_cast<uint4*>((T*)a.y + t * a.ys.t + b * a.ys.b + col[i]) = live ? Piece<T>::pack(f[i]) : zero;
+                if (has[i]) *reinterpret_cast<uint4*>(to + col[i]) = live ? Piece<T>::pack(f[i]) : zero;
         }
     }
 }
@@ -252,12 +289,12 @@ int pow2_at_least(int n) {
     return p;
 }
 
-// The fewest pieces a thread with which a row fits 1024 threads, two where that puts a group into one wave.
+// The fewest pieces a thread with which a row fits the workgroup, two where that puts a group into one wave.
 bool norm_layout(int width, int groups, int vec, NormLayout* out) {
     const int pieces = width / groups / vec;
     for (int vpt = 1; vpt <= NORM_MAX_VPT; vpt *= 2) {
         const int lanes = pow2_at_least((pieces + vpt - 1) / vpt);
-        if ((int64_t)lanes * groups > 1024 || (vpt == 1 && lanes > 64)) continue;
+        if ((int64_t)lanes * groups > NORM_THREADS || (vpt == 1 && lanes > 64)) continue;
         const int slots = lanes * groups;
         // several rows share a workgroup only where each row's sums stay inside a wave
         out->lanes = lanes; out->vpt = vpt; out->slots = slots;
@@ -267,13 +304,28 @@ bool norm_layout(int width, int groups, int vec, NormLayout* out) {
     return false;
 }
 
+template <typename T, int VPT>
+void launch_norm_vpt(const NormArgs& a, unsigned grid, unsigned threads, hipStream_t stream) {
+    switch ((a.after ? 4 : 0) + (a.act ? 2 : 0) + (a.before ? 1 : 0)) {
+    case 0: block_norm_kernel<T, VPT, false, false, false><<<grid, threads, 0, stream>>>(a); break;
+    case 1: block_norm_kernel<T, VPT, false, false, true><<<grid, threads, 0, stream>>>(a); break;
+    case 2: block_norm_kernel<T, VPT, false, true, false><<<grid, threads, 0, stream>>>(a); break;
+    case 3: block_norm_kernel<T, VPT, false, true, true><<<grid, threads, 0, stream>>>(a); break;
+    case 4: block_norm_kernel<T, VPT, true, false, false><<<grid, threads, 0, stream>>>(a); break;
+    case 5: block_norm_kernel<T, VPT, true, false, true><<<grid, threads, 0, stream>>>(a); break;
+    case 6: block_norm_kernel<T, VPT, true, true, false><<<grid, threads, 0, stream>>>(a); break;
+    default: block_norm_kernel<T, VPT, true, true, true><<<grid, threads, 0, stream>>>(a); break;
+    }
+}
+
 template <typename T>
 void launch_norm(const NormArgs& a, unsigned grid, unsigned threads, hipStream_t stream) {
     switch (a.lay.vpt) {
-    case 1: block_norm_kernel<T, 1><<<grid, threads, 0, stream>>>(a); break;
-    case 2: block_norm_kernel<T, 2><<<grid, threads, 0, stream>>>(a); break;
-    case 4: block_norm_kernel<T, 4><<<grid, threads, 0, stream>>>(a); break;
-    default: block_norm_kernel<T, 8><<<grid, threads, 0, stream>>>(a); break;
+    case 1: launch_norm_vpt<T, 1>(a, grid, threads, stream); break;
+    case 2: launch_norm_vpt<T, 2>(a, grid, threads, stream); break;
+    case 4: launch_norm_vpt<T, 4>(a, grid, threads, stream); break;
+    case 8: launch_norm_vpt<T, 8>(a, grid, threads, stream); break;
+    default: launch_norm_vpt<T, 16>(a, grid, threads, stream); break;
     }
 }
 
@@ -401,6 +453,13 @@ int rnn_block_norm_forward(const rnn_block_norm* n, const void* x, const int64_t
     a.aw = n->aw; a.ab = n->ab; a.sc = n->sc; a.bw = n->bw; a.bb = n->bb;
     a.lengths = lengths; a.T = T; a.B = B; a.W = n->W; a.groups = n->groups;
     a.after = n->after; a.before = n->before; a.act = n->gate; a.eps = n->eps; a.lay = n->lay;
+    a.per_group = 1.0f / (n->W / n->groups);
+    a.per_row = 1.0f / n->W;
+    // for row < 2^31 and B <= 2^l: row * (2^(31 + l) / B + 1) >> (31 + l) is row / B
+    uint32_t l = 0;
+    while (((int64_t)1 << l) < B) ++l;
+    a.shift = 31 + l;
+    a.divide = (uint32_t)(((uint64_t)1 << a.shift) / B + 1);
     const int64_t rows = (int64_t)T * B, wgs = (rows + n->lay.rows - 1) / n->lay.rows;
     const unsigned threads = (unsigned)((n->lay.slots * n->lay.rows + 63) / 64 * 64);
     const int64_t most = (int64_t)n->cus * 2048 / threads;             // what the GPU holds at once

@@ -23,7 +23,7 @@ struct LaArgs {
     float* sT;                 // likewise; may be s0
     const float* powers;       // [H, LA_CHUNK + 1]: decay[h]^n
     const double* log2_decay;  // [H]
-    float* seams;              // [pieces - 1, B, H, Dk, Dv] when pieces > 1
+    float* seams;              // [pieces, B, H, Dk, Dv] when pieces > 1: the state that each piece starts from
     float scale;
     int T, B, H, rep;          // rep: heads that share a head of k and v
     int Dk, Dv;
@@ -33,5 +33,73 @@ struct LaArgs {
 
 // linear_attention.hip: one step after the other, for short calls.  wide: 128 columns a workgroup instead of 32.
 hipError_t la_launch_steps(int dtype, const LaArgs& a, bool wide, hipStream_t stream);
+
+// linear_attention_chunk.hip, linear_attention_chunk_f32.hip: chunks of steps by matrix products.  key_tiles, waves: from
+// la_key_tiles and la_waves.  With `states` only the state that each piece but the last adds is computed, into the seams.
+hipError_t la_launch_chunks_bf16(const LaArgs& a, int key_tiles, int waves, bool states, hipStream_t stream);
+hipError_t la_launch_chunks_f32(const LaArgs& a, int key_tiles, int waves, bool states, hipStream_t stream);
+
+// Blocks of 32 rows that a chunk kernel holds of a state, and blocks of 32 columns (waves) of a workgroup.
+inline int la_key_tiles(int Dk) {
+    const int t = (Dk + 31) / 32;
+    return t <= 4 ? t : t <= 6 ? 6 : 8;
+}
+inline int la_waves(int Dk, int Dv) {
+    const int t = (Dv + 31) / 32, blocks = (t + 3) / 4, w = (t + blocks - 1) / blocks;
+    return Dk > 128 ? 4 : w < 2 ? 2 : w;       // rows of wide keys are more than few waves can hold in flight
+}
+
+// Where a workgroup of a chunk kernel works.  Workgroups go to the eight XCDs in turn: those that read the same keys
+// (heads that share them, blocks of columns) follow one another on one XCD, whose L2 then serves all but the first.
+struct LaPlace {
+    int b, h, hk, v0, t0, t1, len, piece;
+};
+
+__device__ inline bool la_place(const LaArgs& a, int pieces, int cols, LaPlace* p) {
+    const int64_t units = (int64_t)a.B * (a.H / a.rep) * pieces;
+    const int shared = a.rep * a.vblocks;
+    const int64_t idx = blockIdx.x / 8, unit = idx / shared * 8 + blockIdx.x % 8;
+    if (unit >= units) return false;
+    const int r = (int)(idx % shared);
+    p->piece = (int)(unit % pieces);
+    p->hk = (int)(unit / pieces % (a.H / a.rep));
+    p->b = (int)(unit / pieces / (a.H / a.rep));
+    p->h = p->hk * a.rep + r / a.vblocks;
+    p->v0 = r % a.vblocks * cols;
+    p->t0 = p->piece * a.piece_steps;
+    p->t1 = min(a.T, p->t0 + a.piece_steps);
+    int len = a.lengths ? a.lengths[p->b] : a.T;
+    p->len = min(max(len, 0), a.T);
+    return true;
+}
+
+inline int64_t la_grid(const LaArgs& a, int pieces) {
+    const int64_t units = (int64_t)a.B * (a.H / a.rep) * pieces;
+    return (units + 7) / 8 * 8 * a.rep * a.vblocks;
+}
+
+// N pieces of 16 bytes a thread of the rows [0, n) of a [ROWS, WIDTH] tile, zeros behind row n and column `width`.
+template <typename T, int ROWS, int WIDTH, int THREADS>
+struct LaTile {
+    static constexpr int VEC = 16 / sizeof(T);
+    static constexpr int PER_ROW = WIDTH / VEC, ALL = ROWS * PER_ROW, N = (ALL + THREADS - 1) / THREADS;
+    static constexpr int STRIDE = WIDTH + VEC;         // of a row in LDS: 16 bytes more, so that rows start in other banks
+    uint4 reg[N];
+    __device__ inline void load(const T* from, int64_t stride, int n, int width) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = threadIdx.x + i * THREADS, row = at / PER_ROW, c = at % PER_ROW * VEC;
+            reg[i] = make_uint4(0, 0, 0, 0);
+            if (row < n && c < width) reg[i] = *reinterpret_cast<const uint4*>(from + row * stride + c);     // n <= ROWS
+        }
+    }
+    __device__ inline void store(T* lds) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = threadIdx.x + i * THREADS, row = at / PER_ROW, c = at % PER_ROW * VEC;
+            if (ALL % THREADS == 0 || at < ALL) *reinterpret_cast<uint4*>(lds + row * STRIDE + c) = reg[i];
+        }
+    }
+};
 
 }  // namespace rnn

@@ -1,4 +1,5 @@
-// Linear attention with a decay for each head: host side, and the kernel that takes one step after the other.
+// Linear attention with a decay for each head: host side, the kernel that takes one step after the other, and the one
+// that joins the pieces of long sequences.
 //
 //   S_t = decay S_{t-1} + k_t v_t^T,   o_t = scale S_t^T q_t        (S [Dk, Dv] fp32, a state for each sequence and head)
 //
@@ -166,18 +167,70 @@ hipError_t la_launch_steps(int dtype, const LaArgs& a, bool wide, hipStream_t st
 
 namespace {
 
+// The pieces of a sequence know what they add to the state; this turns it into the state that each starts from.
+// One thread for four elements of a state; bound by reading and writing the seams once.
+__global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a) {
+    const int64_t per_state = (int64_t)a.Dk * a.Dv, states = (int64_t)a.B * a.H * per_state;
+    const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (i >= states) return;
+    const int64_t unit = i / per_state;                // Dv is a multiple of 4: the four are of one state
+    const int b = (int)(unit / a.H), h = (int)(unit % a.H);
+    const int len = min(a.lengths ? a.lengths[b] : a.T, a.T);
+    const float decay = (float)exp2((double)a.piece_steps * a.log2_decay[h]);
+    float4 run = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (a.s0) {
+        run = *reinterpret_cast<const float4*>(a.s0 + i);
+        *reinterpret_cast<float4*>(a.seams + i) = run;   // the first piece reads it here: sT may be s0
+    }
+    for (int p = 1; p < a.pieces && len > p * a.piece_steps; ++p) {
+        float4* at = reinterpret_cast<float4*>(a.seams + p * states + i);
+        const float4 add = *at;
+        run.x = fmaf(decay, run.x, add.x);
+        run.y = fmaf(decay, run.y, add.y);
+        run.z = fmaf(decay, run.z, add.z);
+        run.w = fmaf(decay, run.w, add.w);
+        *at = run;
+    }
+}
+
+// Workgroups that the pieces of sequences are to make up together: two for each of the 256 compute units.
+constexpr int LA_WORKGROUPS = 512;
+constexpr int LA_FEWEST_STEPS = 32;                // below that, one step after the other
+constexpr int LA_PIECE_STEPS = 256;                // of a piece at least
+
 struct LaPlan {
     int chunk = 0, vblocks = 1, pieces = 1, piece_steps = 0;
     bool wide = false;
 };
 
 LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
-    (void)Dk; (void)dtype;
+    (void)dtype;
     LaPlan p;
-    p.wide = (int64_t)B * H * ((Dv + 127) / 128) >= 512;
-    p.vblocks = p.wide ? (Dv + 127) / 128 : (Dv + 31) / 32;
     p.piece_steps = T;
+    if (T < LA_FEWEST_STEPS) {
+        p.wide = (int64_t)B * H * ((Dv + 127) / 128) >= 512;
+        p.vblocks = p.wide ? (Dv + 127) / 128 : (Dv + 31) / 32;
+        return p;
+    }
+    p.chunk = LA_CHUNK;
+    const int cols = 32 * la_waves(Dk, Dv);
+    p.vblocks = (Dv + cols - 1) / cols;
+    const int64_t units = (int64_t)B * H * p.vblocks;
+    const int64_t want = LA_WORKGROUPS / units, most = T / LA_PIECE_STEPS;
+    const int pieces = (int)(want < most ? want : most);
+    if (pieces >= 2) {
+        const int chunks = (T + LA_CHUNK - 1) / LA_CHUNK;
+        p.piece_steps = (chunks + pieces - 1) / pieces * LA_CHUNK;
+        p.pieces = (T + p.piece_steps - 1) / p.piece_steps;
+    }
+    if (p.pieces == 1) p.piece_steps = T;
     return p;
+}
+
+// Bytes of the seams of any shape: pieces are cut only while B * H * vblocks * pieces stays within LA_WORKGROUPS.
+size_t seam_bytes(int Dk, int Dv) {
+    const int cols = 32 * la_waves(Dk, Dv);
+    return (size_t)(LA_WORKGROUPS / ((Dv + cols - 1) / cols)) * Dk * Dv * sizeof(float);
 }
 
 int check_shape(int H, int Hkv, int Dk, int Dv, int dtype) {
@@ -313,6 +366,20 @@ int rnn_linear_attention_plan_query(int num_heads, int num_kv_heads, int key_siz
 
 int rnn_linear_attention_reserve(rnn_linear_attention* l, int T, int B) {
     if (!l || T < 1 || B < 1) return RNN_EINVAL;
+    if (l->seams || choose(l->H, l->Dk, l->Dv, l->dtype, T, B).pieces == 1) return RNN_OK;
+    int device = -1;
+    if (hipGetDevice(&device) != hipSuccess) {
+        (void)hipGetLastError();
+        return RNN_EDEVICE;
+    }
+    if (device != l->device) return RNN_EINVAL;
+    const size_t bytes = seam_bytes(l->Dk, l->Dv);
+    if (hipMalloc((void**)&l->seams, bytes) != hipSuccess) {
+        (void)hipGetLastError();
+        l->seams = nullptr;
+        return RNN_ENOMEM;
+    }
+    l->seam_bytes = bytes;
     return RNN_OK;
 }
 
@@ -338,13 +405,40 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
         return RNN_EDEVICE;
     }
     if (device != l->device) return RNN_EINVAL;
+    const hipStream_t st = (hipStream_t)stream;
+    if (p.pieces > 1 && !l->seams) {
+        hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+        if (hipStreamIsCapturing(st, &cap) != hipSuccess) {
+            (void)hipGetLastError();
+            return RNN_EDEVICE;
+        }
+        if (cap != hipStreamCaptureStatusNone) return RNN_EUNSUPPORTED;    // nothing can be allocated while recording
+        const int held = rnn_linear_attention_reserve(l, T, B);
+        if (held != RNN_OK) return held;
+    }
     a.q = q; a.k = k; a.v = v; a.o = o;
     a.lengths = lengths; a.s0 = s0; a.sT = sT;
     a.powers = l->powers; a.log2_decay = l->log2_decay; a.seams = l->seams;
     a.scale = l->scale;
     a.T = T; a.B = B; a.H = l->H; a.rep = l->H / l->Hkv; a.Dk = l->Dk; a.Dv = l->Dv;
     a.vblocks = p.vblocks; a.pieces = p.pieces; a.piece_steps = p.piece_steps;
-    return la_launch_steps(l->dtype, a, p.wide, (hipStream_t)stream) == hipSuccess ? RNN_OK : RNN_EDEVICE;
+    hipError_t e = hipSuccess;
+    if (!p.chunk) {
+        e = la_launch_steps(l->dtype, a, p.wide, st);
+    } else {
+        const auto chunks = l->dtype == RNN_BF16 ? la_launch_chunks_bf16 : la_launch_chunks_f32;
+        const int kt = la_key_tiles(l->Dk), nw = la_waves(l->Dk, l->Dv);
+        if (p.pieces > 1) {
+            e = chunks(a, kt, nw, true, st);
+            if (e == hipSuccess) {
+                const int64_t quads = (int64_t)B * l->H * l->Dk * l->Dv / 4;       // few: pieces are cut where heads are
+                la_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a);
+                e = hipGetLastError();
+            }
+        }
+        if (e == hipSuccess) e = chunks(a, kt, nw, false, st);
+    }
+    return e == hipSuccess ? RNN_OK : RNN_EDEVICE;
 }
 
 }  // extern "C"
