@@ -5,25 +5,30 @@
 // One pass: a row is read once into registers, every mean is taken from there (the variance from the differences to the
 // mean, so nothing cancels), and what is asked for is written once.  Bound by the bytes of its tensors.
 //
-// A thread holds VPT pieces of 16 bytes of a row.  `lanes` threads hold one group: a power of two, so that a group's sums stay
-// inside a wave or take whole waves.  The parts that a norm lacks are compiled out (AFTER, GATE, BEFORE): at some twenty
-// vector instructions an element the arithmetic would take as long as the bytes.
+// Layout.  A row is a line of slots, one piece of 16 bytes each (or three of one group); thread i of the row's `waves`
+// waves holds slots i, i + 64 waves, .. (VPT pieces in all).  A group starts a power of two of slots, or a whole number of 64, so that 64 neighbouring
+// slots, which a wave sums up with cross-lane instructions, hold whole groups or belong to one.  Rows of one wave need
+// no barrier: 65536 rows of 2048 bf16 values, sum and norm, take 204 us with one wave of four pieces a thread, 219 us with
+// two waves and a barrier for the sum.
+// The parts that a norm lacks are compiled out (AFTER, GATE, BEFORE).
 #include "../../include/rnn.h"
 #include "common.h"
 
 #include <cmath>
-#include <cstring>
 #include <new>
 
 namespace rnn {
 namespace {
 
 constexpr int NORM_MAX_WIDTH = 16384;
-constexpr int NORM_MAX_VPT = 16;
-constexpr int NORM_THREADS = 512;
+constexpr int NORM_WAVES = 8;                      // of a workgroup at most
+constexpr int NORM_CHUNKS = 128;                   // of 64 slots in a row at most
 
 struct NormLayout {
-    int lanes, vpt, slots, rows;   // threads of a group, pieces of a thread, threads of a row, rows of a workgroup
+    int lanes, slots;    // threads of a group, of a row
+    int deep;            // neighbouring pieces of a thread that belong to one group
+    int waves, vpt;      // waves of a row, pieces of a thread
+    int rows;            // of a workgroup; more than 4: several in a wave
 };
 
 struct RowView {
@@ -46,7 +51,8 @@ struct NormArgs {
     int T, B, W, groups;
     int after, before, act;
     float eps, per_group, per_row;   // 1 / width of a group, of a row
-    uint32_t divide, shift;          // row / B = row * divide >> shift
+    bool by_sequence;                // rows are taken in the order [B, T] instead of [T, B]: that of x in memory
+    uint32_t inner, divide, shift;   // the inner one of T and B; row / inner = row * divide >> shift
     NormLayout lay;
 };
 
@@ -95,45 +101,86 @@ __device__ inline float sum_in_wave(float v, int lanes) {
     if (lanes >= 4) v = plus_dpp<0x4E>(v);             // quad_perm [2, 3, 0, 1]
     if (lanes >= 8) v = plus_dpp<0x141>(v);            // row_half_mirror: the other four of eight
     if (lanes >= 16) v = plus_dpp<0x140>(v);           // row_mirror: the other eight of sixteen
-    if (lanes >= 32) v += __shfl_xor(v, 16);
-    if (lanes >= 64) v += __shfl_xor(v, 32);
+    if (lanes >= 32) {                                 // the other sixteen of thirty-two
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
+    if (lanes >= 64) {                                 // the other half of the wave
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+    }
     return v;
 }
 
-// Sums that may cross waves; each uses the buffer that the one before did not, so that one barrier a sum is enough.
+// Sums of a row's numbers.  Those that cross waves use two buffers in turn, so that one barrier a sum is enough.
+template <int VPT>
 struct Sums {
-    float (*buf)[16];
+    float (*buf)[NORM_CHUNKS];
     int turn;
-    // over the `lanes` threads of a group: inside a wave, or whole waves
-    __device__ inline float group(float v, int lanes) {
-        v = sum_in_wave(v, min(lanes, 64));
-        if (lanes <= 64) return v;
-        const int n = lanes >> 6, first = (threadIdx.x >> 6) & -n;
-        return across(v, first, n);
-    }
-    // over the threads of a row: inside a wave, or the workgroup
-    __device__ inline float row(float v, int slots, int waves) {
-        if ((slots & (slots - 1)) == 0 && slots <= 64) return sum_in_wave(v, slots);
-        return across(sum_in_wave(v, 64), 0, waves);
-    }
-    __device__ inline float across(float v, int first, int n) {
+    // of all: `lanes` threads in a wave, or all threads of `waves` waves
+    __device__ inline float row(float v, int lanes, int waves) {
+        v = sum_in_wave(v, lanes);
+        if (waves == 1) return v;
         float* b = buf[turn];
         turn ^= 1;
         if ((threadIdx.x & 63) == 0) b[threadIdx.x >> 6] = v;
         __syncthreads();
         float s = 0.f;
-        for (int w = 0; w < n; ++w) s += b[first + w];
+        for (int w = 0; w < waves; ++w) s += b[w];
         return s;
+    }
+    // of each group; v[i]: what the thread has of slot i's group, replaced by that group's sum
+    __device__ inline void groups(float (&v)[VPT], int lanes, int waves, int deep) {
+        if (deep > 1) {                                // slots of whole groups; pieces behind a multiple of deep are none
+#pragma unroll
+            for (int i = 1; i < VPT; ++i) v[i] += i % deep ? v[i - 1] : 0.f;
+#pragma unroll
+            for (int i = VPT - 1; i >= 0; --i)
+                if (i % deep == deep - 1) v[i] = sum_in_wave(v[i], min(lanes, 64));
+#pragma unroll
+            for (int i = VPT - 2; i >= 0; --i) v[i] = i % deep == deep - 1 ? v[i] : v[i + 1];
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) v[i] = sum_in_wave(v[i], min(lanes, 64));
+        const int chunks = lanes >> 6;                 // 64 slots each that a group takes
+        if (chunks <= 1) return;
+        float s[VPT];
+        if (waves == 1) {
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                s[i] = 0.f;
+#pragma unroll
+                for (int j = 0; j < VPT; ++j) s[i] += i / chunks == j / chunks ? v[j] : 0.f;
+            }
+        } else {
+            float* b = buf[turn];
+            turn ^= 1;
+            const int wave = threadIdx.x >> 6;
+            if ((threadIdx.x & 63) == 0) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) b[i * waves + wave] = v[i];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) {
+                const int first = (i * waves + wave) / chunks * chunks;
+                s[i] = 0.f;
+                for (int j = first; j < min(first + chunks, VPT * waves); ++j) s[i] += b[j];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VPT; ++i) v[i] = s[i];
     }
 };
 
 template <typename T, int VPT>
-__device__ inline void normalise(float (&f)[VPT][Piece<T>::N], float factor, const T* w, const T* c, const int* col, const bool* has) {
+__device__ inline void normalise(float (&f)[VPT][Piece<T>::N], const float* factor, const T* w, const T* c, const int* col, const bool* has) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         float x[Piece<T>::N];
 #pragma unroll
-        for (int e = 0; e < Piece<T>::N; ++e) f[i][e] *= factor;
+        for (int e = 0; e < Piece<T>::N; ++e) f[i][e] *= factor[i];
         if (w && has[i]) {
             Piece<T>::unpack(*reinterpret_cast<const uint4*>(w + col[i]), x);
 #pragma unroll
@@ -147,14 +194,17 @@ __device__ inline void normalise(float (&f)[VPT][Piece<T>::N], float factor, con
     }
 }
 
-template <typename T, int VPT, bool AFTER, bool GATE, bool BEFORE>
-__global__ __launch_bounds__(NORM_THREADS) void block_norm_kernel(const NormArgs a) {
+// WAVE_ROW: all threads of a wave have the same row, whose place is then found by the scalar unit.
+template <typename T, int VPT, bool AFTER, bool GATE, bool BEFORE, bool WAVE_ROW>
+__global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormArgs a) {
     constexpr int N = Piece<T>::N;
-    __shared__ float buf[2][16];
-    Sums sums = {buf, 0};
-    const int waves = blockDim.x >> 6;
-    const int slot = threadIdx.x % (unsigned)a.lay.slots, sub = threadIdx.x / (unsigned)a.lay.slots;
-    const int group = slot / (unsigned)a.lay.lanes, lane = slot % (unsigned)a.lay.lanes;
+    __shared__ float buf[2][NORM_CHUNKS];
+    Sums<VPT> sums;
+    sums.buf = buf;
+    sums.turn = 0;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int waves = WAVE_ROW ? a.lay.waves : 1, row_lanes = WAVE_ROW ? 64 : a.lay.slots;
+    const int sub = WAVE_ROW ? __builtin_amdgcn_readfirstlane(waves == 1 ? wave : 0) : threadIdx.x / (unsigned)a.lay.slots;
     const int gw = a.W / a.groups;                      // width of a group
     const uint4 zero = make_uint4(0, 0, 0, 0);
 
@@ -162,18 +212,23 @@ __global__ __launch_bounds__(NORM_THREADS) void block_norm_kernel(const NormArgs
     bool has[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
-        const int c = (i * a.lay.lanes + lane) * N;
-        has[i] = c < gw && sub < a.lay.rows;
+        const unsigned pass = i / (unsigned)a.lay.deep, in_group = i % (unsigned)a.lay.deep;
+        const unsigned slot = WAVE_ROW ? (pass * waves + (waves == 1 ? 0 : wave)) * 64 + lane : threadIdx.x % (unsigned)a.lay.slots;
+        const unsigned group = slot / (unsigned)a.lay.lanes, c = (slot % (unsigned)a.lay.lanes + in_group * a.lay.lanes) * N;
+        has[i] = (int)c < gw && (int)group < a.groups;
         col[i] = has[i] ? group * gw + c : 0;
     }
 
     const uint32_t rows = (uint32_t)a.T * a.B, step = gridDim.x * a.lay.rows;        // at most 2^30 and 2^21
-    for (uint32_t r0 = blockIdx.x * a.lay.rows; r0 < rows; r0 += step) {
-        const uint32_t row = r0 + sub;
-        const bool in = sub < a.lay.rows && row < rows;
-        const uint32_t t = in ? (uint32_t)(((uint64_t)row * a.divide) >> a.shift) : 0, b = in ? row - t * a.B : 0;
-        const bool live = in && (!a.lengths || (int)t < a.lengths[b]);
-        uint4 px[VPT], pg[VPT], pr[VPT];
+    uint4 px[VPT], pg[VPT], pr[VPT];
+    uint32_t t, b;
+    bool in, live;
+    auto load = [&](uint32_t row) {
+        in = row < rows;
+        const uint32_t outer = in ? (uint32_t)(((uint64_t)row * a.divide) >> a.shift) : 0, inner = in ? row - outer * a.inner : 0;
+        t = a.by_sequence ? inner : outer;
+        b = a.by_sequence ? outer : inner;
+        live = in && (!a.lengths || (int)t < a.lengths[b]);
         const T* x = (const T*)a.x + t * a.xs.t + b * a.xs.b;
         const T* gate = GATE ? (const T*)a.gate + t * a.gs.t + b * a.gs.b : nullptr;
         const T* residual = a.residual ? (const T*)a.residual + t * a.rs.t + b * a.rs.b : nullptr;
@@ -185,29 +240,58 @@ __global__ __launch_bounds__(NORM_THREADS) void block_norm_kernel(const NormArgs
             if (GATE) pg[i] = *reinterpret_cast<const uint4*>(gate + col[i]);
             if (a.residual) pr[i] = *reinterpret_cast<const uint4*>(residual + col[i]);
         }
+    };
+    for (uint32_t r0 = blockIdx.x * a.lay.rows; r0 < rows; r0 += step) {
+        load(r0 + sub);
+        if (WAVE_ROW && !live) {                           // a wave's rows, and with barriers a workgroup's, are one
+            if (in) {
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) {
+                    if (!has[i]) continue;
+                    if (a.residual_out) *reinterpret_cast<uint4*>((T*)a.residual_out + t * a.os.t + b * a.os.b + col[i]) = zero;
+                    if (a.y) *reinterpret_cast<uint4*>((T*)a.y + t * a.ys.t + b * a.ys.b + col[i]) = zero;
+                }
+            }
+            continue;
+        }
         float f[VPT][N];
 #pragma unroll
         for (int i = 0; i < VPT; ++i) Piece<T>::unpack(px[i], f[i]);
 
         if (AFTER) {
-            float s = 0.f;
+            float s[VPT];
+            auto sum = [&]() {
+                if (a.groups > 1) return sums.groups(s, a.lay.lanes, waves, a.lay.deep);
+                float all = 0.f;
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) all += s[i];
+                all = sums.row(all, row_lanes, waves);
+#pragma unroll
+                for (int i = 0; i < VPT; ++i) s[i] = all;
+            };
             if (a.after == RNN_NORM_LAYER) {
 #pragma unroll
+                for (int i = 0; i < VPT; ++i) {
+                    s[i] = 0.f;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) s[i] += f[i][e];       // pieces behind the group are zero
+                }
+                sum();
+#pragma unroll
                 for (int i = 0; i < VPT; ++i)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) s += f[i][e];         // pieces behind the group are zero
-                const float mean = sums.group(s, a.lay.lanes) * a.per_group;
-#pragma unroll
-                for (int i = 0; i < VPT; ++i)
-#pragma unroll
-                    for (int e = 0; e < N; ++e) f[i][e] = has[i] ? f[i][e] - mean : 0.f;
-                s = 0.f;
+                    for (int e = 0; e < N; ++e) f[i][e] = has[i] ? f[i][e] - s[i] * a.per_group : 0.f;
             }
 #pragma unroll
-            for (int i = 0; i < VPT; ++i)
+            for (int i = 0; i < VPT; ++i) {
+                s[i] = 0.f;
 #pragma unroll
-                for (int e = 0; e < N; ++e) s = fmaf(f[i][e], f[i][e], s);
-            normalise<T, VPT>(f, 1.0f / sqrtf(sums.group(s, a.lay.lanes) * a.per_group + a.eps), (const T*)a.aw, (const T*)a.ab, col, has);
+                for (int e = 0; e < N; ++e) s[i] = fmaf(f[i][e], f[i][e], s[i]);
+            }
+            sum();
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) s[i] = 1.0f / sqrtf(s[i] * a.per_group + a.eps);
+            normalise<T, VPT>(f, s, (const T*)a.aw, (const T*)a.ab, col, has);
         }
         if (GATE) {
 #pragma unroll
@@ -253,26 +337,28 @@ __global__ __launch_bounds__(NORM_THREADS) void block_norm_kernel(const NormArgs
         }
         if (!a.y) continue;                                // the same for all threads
         if (BEFORE) {
-            // pieces behind the group may hold a bias by now
             float s = 0.f;
             if (a.before == RNN_NORM_LAYER) {
 #pragma unroll
                 for (int i = 0; i < VPT; ++i)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) s += has[i] ? f[i][e] : 0.f;
-                const float mean = sums.row(s, a.lay.slots, waves) * a.per_row;
+                    for (int e = 0; e < N; ++e) s += f[i][e];         // pieces behind a group are zero, whatever was done to them
+                const float mean = sums.row(s, row_lanes, waves) * a.per_row;
 #pragma unroll
                 for (int i = 0; i < VPT; ++i)
 #pragma unroll
-                    for (int e = 0; e < N; ++e) f[i][e] -= mean;
+                    for (int e = 0; e < N; ++e) f[i][e] = has[i] ? f[i][e] - mean : 0.f;
                 s = 0.f;
             }
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
-                if (has[i])
 #pragma unroll
-                    for (int e = 0; e < N; ++e) s = fmaf(f[i][e], f[i][e], s);
-            normalise<T, VPT>(f, 1.0f / sqrtf(sums.row(s, a.lay.slots, waves) * a.per_row + a.eps), (const T*)a.bw, (const T*)a.bb, col, has);
+                for (int e = 0; e < N; ++e) s = fmaf(f[i][e], f[i][e], s);
+            float factor[VPT];
+            s = 1.0f / sqrtf(sums.row(s, row_lanes, waves) * a.per_row + a.eps);
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) factor[i] = s;
+            normalise<T, VPT>(f, factor, (const T*)a.bw, (const T*)a.bb, col, has);
         }
         if (in) {
             T* to = (T*)a.y + t * a.ys.t + b * a.ys.b;
@@ -289,43 +375,64 @@ int pow2_at_least(int n) {
     return p;
 }
 
-// The fewest pieces a thread with which a row fits the workgroup, two where that puts a group into one wave.
-bool norm_layout(int width, int groups, int vec, NormLayout* out) {
-    const int pieces = width / groups / vec;
-    for (int vpt = 1; vpt <= NORM_MAX_VPT; vpt *= 2) {
-        const int lanes = pow2_at_least((pieces + vpt - 1) / vpt);
-        if ((int64_t)lanes * groups > NORM_THREADS || (vpt == 1 && lanes > 64)) continue;
-        const int slots = lanes * groups;
-        // several rows share a workgroup only where each row's sums stay inside a wave
-        out->lanes = lanes; out->vpt = vpt; out->slots = slots;
-        out->rows = (slots <= 64 && (slots & (slots - 1)) == 0) ? 256 / slots : 1;
-        return true;
-    }
-    return false;
+// The slots of a row.  Groups of some widths would leave many slots empty, of ten pieces six; three pieces to a slot leave two
+// of twelve (33000 rows of 26 groups of 80 bf16 values: 127 us against 156).
+bool norm_slots(int width, int groups, int vec, NormLayout* out) {
+    const int pieces = width / groups / vec, third = (pieces + 2) / 3;
+    out->deep = groups > 1 && pieces <= 64 && 5 * pow2_at_least(pieces) >= 6 * 3 * pow2_at_least(third) ? 3 : 1;
+    const int l = out->deep == 3 ? third : pieces;
+    out->lanes = l <= 32 || (groups > 1 && l <= 64) ? pow2_at_least(l) : (l + 63) / 64 * 64;
+    out->slots = out->lanes * groups;
+    return out->slots <= 64 * NORM_CHUNKS;
 }
 
-template <typename T, int VPT>
+// How `rows` rows are divided.  Rows that are few are spread over as many waves as they have pieces for, until there is
+// a wave for every SIMD of the GPU (64 rows of 1024 bf16 values: 3.7 us with one piece a thread, 4.3 with two, 5.1 with four).
+// Many rows take as few waves each as hold four pieces a thread (five of fp32), and three with a norm by groups, whose
+// registers would leave too few waves a SIMD (17157 padded rows of 1280 fp32 values, everything at once: 98 us with
+// three, 110 with five; 65536 rows of 16 gated heads of 128: 168 with two, 181 with four).
+void norm_divide(NormLayout* l, int64_t rows, int vec, bool after, int simds) {
+    if (l->slots <= 32 && (l->slots & (l->slots - 1)) == 0 && l->deep == 1) {
+        l->waves = l->vpt = 1;
+        l->rows = 256 / l->slots;
+        return;
+    }
+    const int chunks = (l->slots + 63) / 64, most = after ? 3 / l->deep : vec == 4 ? 5 : 4;
+    int w = (chunks + most - 1) / most;
+    while (w < chunks && w < NORM_WAVES && rows * w < simds) ++w;
+    if (w > NORM_WAVES) w = NORM_WAVES;
+    l->waves = w;
+    l->vpt = (chunks + w - 1) / w * l->deep;
+    l->rows = w == 1 ? 4 : 1;
+}
+
+template <typename T, int VPT, bool WAVE_ROW>
 void launch_norm_vpt(const NormArgs& a, unsigned grid, unsigned threads, hipStream_t stream) {
     switch ((a.after ? 4 : 0) + (a.act ? 2 : 0) + (a.before ? 1 : 0)) {
-    case 0: block_norm_kernel<T, VPT, false, false, false><<<grid, threads, 0, stream>>>(a); break;
-    case 1: block_norm_kernel<T, VPT, false, false, true><<<grid, threads, 0, stream>>>(a); break;
-    case 2: block_norm_kernel<T, VPT, false, true, false><<<grid, threads, 0, stream>>>(a); break;
-    case 3: block_norm_kernel<T, VPT, false, true, true><<<grid, threads, 0, stream>>>(a); break;
-    case 4: block_norm_kernel<T, VPT, true, false, false><<<grid, threads, 0, stream>>>(a); break;
-    case 5: block_norm_kernel<T, VPT, true, false, true><<<grid, threads, 0, stream>>>(a); break;
-    case 6: block_norm_kernel<T, VPT, true, true, false><<<grid, threads, 0, stream>>>(a); break;
-    default: block_norm_kernel<T, VPT, true, true, true><<<grid, threads, 0, stream>>>(a); break;
+    case 0: block_norm_kernel<T, VPT, false, false, false, WAVE_ROW><<<grid, threads, 0, stream>>>(a); break;
+    case 1: block_norm_kernel<T, VPT, false, false, true, WAVE_ROW><<<grid, threads, 0, stream>>>(a); break;
+    case 2: block_norm_kernel<T, VPT, false, true, false, WAVE_ROW><<<grid, threads, 0, stream>>>(a); break;
+    case 3: block_norm_kernel<T, VPT, false, true, true, WAVE_ROW><<<grid, threads, 0, stream>>>(a); break;
+    case 4: block_norm_kernel<T, VPT, true, false, false, WAVE_ROW><<<grid, threads, 0, stream>>>(a); break;
+    case 5: block_norm_kernel<T, VPT, true, false, true, WAVE_ROW><<<grid, threads, 0, stream>>>(a); break;
+    case 6: block_norm_kernel<T, VPT, true, true, false, WAVE_ROW><<<grid, threads, 0, stream>>>(a); break;
+    default: block_norm_kernel<T, VPT, true, true, true, WAVE_ROW><<<grid, threads, 0, stream>>>(a); break;
     }
 }
 
 template <typename T>
 void launch_norm(const NormArgs& a, unsigned grid, unsigned threads, hipStream_t stream) {
+    if (a.lay.rows > 4) return launch_norm_vpt<T, 1, false>(a, grid, threads, stream);
     switch (a.lay.vpt) {
-    case 1: launch_norm_vpt<T, 1>(a, grid, threads, stream); break;
-    case 2: launch_norm_vpt<T, 2>(a, grid, threads, stream); break;
-    case 4: launch_norm_vpt<T, 4>(a, grid, threads, stream); break;
-    case 8: launch_norm_vpt<T, 8>(a, grid, threads, stream); break;
-    default: launch_norm_vpt<T, 16>(a, grid, threads, stream); break;
+    case 1: launch_norm_vpt<T, 1, true>(a, grid, threads, stream); break;
+    case 2: launch_norm_vpt<T, 2, true>(a, grid, threads, stream); break;
+    case 3: launch_norm_vpt<T, 3, true>(a, grid, threads, stream); break;
+    case 4: launch_norm_vpt<T, 4, true>(a, grid, threads, stream); break;
+    case 5: launch_norm_vpt<T, 5, true>(a, grid, threads, stream); break;
+    case 6: launch_norm_vpt<T, 6, true>(a, grid, threads, stream); break;
+    case 7:
+    case 8: launch_norm_vpt<T, 8, true>(a, grid, threads, stream); break;
+    default: launch_norm_vpt<T, 16, true>(a, grid, threads, stream); break;
     }
 }
 
@@ -380,8 +487,8 @@ int rnn_block_norm_create(rnn_block_norm** out, int width, int dtype, int after,
     if (after == RNN_NORM_NONE) groups = 1;        // nothing is done by groups
     if (width > NORM_MAX_WIDTH || width % vec != 0 || (width / groups) % vec != 0 || (groups > 1 && width / groups < 32))
         return RNN_EUNSUPPORTED;
-    NormLayout lay;
-    if (!norm_layout(width, groups, vec, &lay)) return RNN_EUNSUPPORTED;
+    NormLayout lay = {};
+    if (!norm_slots(width, groups, vec, &lay)) return RNN_EUNSUPPORTED;
     rnn_block_norm* n = new rnn_block_norm();
     n->W = width; n->dtype = dtype; n->after = after; n->groups = groups; n->gate = gate; n->before = before; n->eps = eps;
     n->lay = lay;
@@ -455,13 +562,17 @@ int rnn_block_norm_forward(const rnn_block_norm* n, const void* x, const int64_t
     a.after = n->after; a.before = n->before; a.act = n->gate; a.eps = n->eps; a.lay = n->lay;
     a.per_group = 1.0f / (n->W / n->groups);
     a.per_row = 1.0f / n->W;
-    // for row < 2^31 and B <= 2^l: row * (2^(31 + l) / B + 1) >> (31 + l) is row / B
+    a.by_sequence = a.xs.t < a.xs.b;
+    a.inner = a.by_sequence ? T : B;
+    // for row < 2^31 and n <= 2^l: row * (2^(31 + l) / n + 1) >> (31 + l) is row / n
     uint32_t l = 0;
-    while (((int64_t)1 << l) < B) ++l;
+    while (((int64_t)1 << l) < a.inner) ++l;
     a.shift = 31 + l;
-    a.divide = (uint32_t)(((uint64_t)1 << a.shift) / B + 1);
-    const int64_t rows = (int64_t)T * B, wgs = (rows + n->lay.rows - 1) / n->lay.rows;
-    const unsigned threads = (unsigned)((n->lay.slots * n->lay.rows + 63) / 64 * 64);
+    a.divide = (uint32_t)(((uint64_t)1 << a.shift) / a.inner + 1);
+    const int64_t rows = (int64_t)T * B;
+    norm_divide(&a.lay, rows, step, n->after != RNN_NORM_NONE, 4 * n->cus);
+    const int64_t wgs = (rows + a.lay.rows - 1) / a.lay.rows;
+    const unsigned threads = a.lay.rows > 4 ? 256 : 64 * a.lay.waves * a.lay.rows;
     const int64_t most = (int64_t)n->cus * 2048 / threads;             // what the GPU holds at once
     const unsigned grid = (unsigned)(wgs < most ? wgs : most);
     if (n->dtype == RNN_BF16) launch_norm<bf16_t>(a, grid, threads, (hipStream_t)stream);
