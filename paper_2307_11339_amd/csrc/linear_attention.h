@@ -78,26 +78,47 @@ inline int64_t la_grid(const LaArgs& a, int pieces) {
     return (units + 7) / 8 * 8 * a.rep * a.vblocks;
 }
 
-// N pieces of 16 bytes a thread of the rows [0, n) of a [ROWS, WIDTH] tile, zeros behind row n and column `width`.
+// The rows [0, n) of a [ROWS, WIDTH] tile on their way from memory to LDS, N pieces of 16 bytes a thread, zeros behind row n
+// and column `width`.  A thread's pieces stand in one column, AT_ONCE rows apart: one address, and scalar offsets to it.
+// Every thread loads, what is not there from a place that is, and the zeros are put in on the way to LDS: a load under a
+// condition would make the wave wait for it at once, where the two ways meet.
 template <typename T, int ROWS, int WIDTH, int THREADS>
 struct LaTile {
     static constexpr int VEC = 16 / sizeof(T);
-    static constexpr int PER_ROW = WIDTH / VEC, ALL = ROWS * PER_ROW, N = (ALL + THREADS - 1) / THREADS;
+    static constexpr int PER_ROW = WIDTH / VEC, AT_ONCE = THREADS / PER_ROW, N = (ROWS + AT_ONCE - 1) / AT_ONCE;
     static constexpr int STRIDE = WIDTH + VEC;         // of a row in LDS: 16 bytes more, so that rows start in other banks
     uint4 reg[N];
-    __device__ inline void load(const T* from, int64_t stride, int n, int width) {
+    const T* from;
+    int row, at;                                       // of the first piece: its row, its place in LDS
+    bool spare, beyond, part;                          // threads and columns that the tile does not have, whether there are such columns
+    __device__ inline void init(const T* base, int width) {
+        const int c = threadIdx.x % PER_ROW * VEC;
+        row = threadIdx.x / PER_ROW;
+        spare = THREADS % PER_ROW && row >= AT_ONCE;
+        if (spare) row = 0;
+        beyond = c >= width;
+        part = width < WIDTH;
+        at = row * STRIDE + c;
+        from = base + (beyond ? 0 : c);
+    }
+    // offset: of the tile's first row; n >= 1
+    __device__ inline void load(int64_t offset, int64_t stride, int n) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const int at = threadIdx.x + i * THREADS, row = at / PER_ROW, c = at % PER_ROW * VEC;
-            reg[i] = make_uint4(0, 0, 0, 0);
-            if (row < n && c < width) reg[i] = *reinterpret_cast<const uint4*>(from + row * stride + c);     // n <= ROWS
+            const int r = min(row + i * AT_ONCE, n - 1);
+            reg[i] = *reinterpret_cast<const uint4*>(from + offset + r * stride);
         }
     }
-    __device__ inline void store(T* lds) const {
+    __device__ inline void store(T* lds, int n) {
+        if (n < ROWS || part) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int at = threadIdx.x + i * THREADS, row = at / PER_ROW, c = at % PER_ROW * VEC;
-            if (ALL % THREADS == 0 || at < ALL) *reinterpret_cast<uint4*>(lds + row * STRIDE + c) = reg[i];
+            for (int i = 0; i < N; ++i)
+                if (beyond || row + i * AT_ONCE >= n) reg[i] = make_uint4(0, 0, 0, 0);
+        }
+        if (!spare) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if ((i + 1) * AT_ONCE <= ROWS || row + i * AT_ONCE < ROWS) *reinterpret_cast<uint4*>(lds + at + i * AT_ONCE * STRIDE) = reg[i];
         }
     }
 };

@@ -47,25 +47,29 @@ __device__ inline bf16x8 read_transposed(const bf16_t* at, int stride) {
     return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
-// x = hi + mid + lo up to 2^-24 of it; a rest that is no number counts nothing
-__device__ inline void split3(const float* x, bf16x8& hi, bf16x8& mid, bf16x8& lo) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        hi[i] = (__bf16)x[i];
-        float rest = x[i] - (float)hi[i];
-        rest = finite((float)hi[i]) ? rest : 0.f;
-        mid[i] = (__bf16)rest;
-        lo[i] = (__bf16)(rest - (float)mid[i]);
-    }
+// Two numbers rounded to bf16 (nearest, even) in one word, and what the rounding took.
+__device__ inline uint32_t round2(float& x, float& y) {
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+    union { bf16x2 h; uint32_t u; } r;
+    r.h = __builtin_convertvector((f32x2){x, y}, bf16x2);
+    x -= __uint_as_float(r.u << 16);
+    y -= __uint_as_float(r.u & 0xffff0000u);
+    return r.u;
 }
 
-// x = hi + lo up to 2^-16 of it
-__device__ inline void split(const float* x, bf16x8& hi, bf16x8& lo) {
+// x = the sum of PARTS bf16 numbers up to 2^(-8 PARTS) of it
+template <int PARTS>
+__device__ inline void split(const float* x, bf16x8 (&part)[PARTS]) {
+    union { bf16x8 v; uint32_t u[4]; } out[PARTS];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        hi[i] = (__bf16)x[i];
-        lo[i] = (__bf16)(x[i] - (float)hi[i]);
+    for (int i = 0; i < 4; ++i) {
+        float a = x[2 * i], b = x[2 * i + 1];
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) out[p].u[i] = round2(a, b);
     }
+#pragma unroll
+    for (int p = 0; p < PARTS; ++p) part[p] = out[p].v;
 }
 
 template <int KT, int NW, bool STATES>
@@ -110,42 +114,57 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
     if (!STATES && live > 0) from = at.piece > 0 || (a.pieces > 1 && a.s0) ? a.seams + at.piece * states : a.s0;
     if (!STATES && live == 0 && at.piece == 0) from = a.s0;
     f32x16 S[KT];
+    if (from) {
+        // all loads at once, of a place that is there where the state has none
+        const float* col = from + state_at - first_row * (int64_t)a.Dv + (my_col < cols ? 0 : -my_col);
 #pragma unroll
-    for (int x = 0; x < KT; ++x)
+        for (int x = 0; x < KT; ++x)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int row = 32 * x + 16 * (e >> 3) + (e & 7);
-            S[x][e] = 0.f;
-            if (from && my_col < cols && first_row + row < a.Dk) S[x][e] = from[state_at + (int64_t)row * a.Dv];
-        }
+            for (int e = 0; e < 16; ++e) S[x][e] = col[(int64_t)min(first_row + 32 * x + 16 * (e >> 3) + (e & 7), a.Dk - 1) * a.Dv];
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[x][e] = my_col < cols && first_row + 32 * x + 16 * (e >> 3) + (e & 7) < a.Dk ? S[x][e] : 0.f;
+    } else {
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[x][e] = 0.f;
+    }
 
     KeyTile tq, tk;
     ValueTile tv;
+    if (!STATES) tq.init(q, a.Dk);
+    tk.init(k, a.Dk);
+    tv.init(v, cols);
     auto load = [&](int c) {
         const int n = min(C, live - c * C);
-        if (!STATES) tq.load(q + (int64_t)c * C * a.qs.t, a.qs.t, n, a.Dk);
-        tk.load(k + (int64_t)c * C * a.ks.t, a.ks.t, n, a.Dk);
-        tv.load(v + (int64_t)c * C * a.vs.t, a.vs.t, n, cols);
+        if (!STATES) tq.load((int64_t)c * C * a.qs.t, a.qs.t, n);
+        tk.load((int64_t)c * C * a.ks.t, a.ks.t, n);
+        tv.load((int64_t)c * C * a.vs.t, a.vs.t, n);
     };
     auto store = [&](int c) {
         const int n = min(C, live - c * C);
-        if (!STATES) tq.store(sq);
-        tk.store(sk);
-        tv.store(sv);
-        if (tid < C) weight[tid] = tid < n ? power[n - 1 - tid] : 0.f;
+        if (!STATES) tq.store(sq, n);
+        tk.store(sk, n);
+        tv.store(sv, n);
+        if (c == 0 || n < C) {
+            if (tid < C) weight[tid] = tid < n ? power[n - 1 - tid] : 0.f;
+        }
         if (!STATES) {
-            uint32_t bad = 0;
+            uint32_t bad = 0;          // an exponent of ones carries into the sign
 #pragma unroll
             for (int i = 0; i < ValueTile::N; ++i) {
-                const uint32_t u[4] = {tv.reg[i].x, tv.reg[i].y, tv.reg[i].z, tv.reg[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    bad |= (uint32_t)((u[j] & 0x7f80u) == 0x7f80u) | (uint32_t)((u[j] & 0x7f800000u) == 0x7f800000u);
+                bad |= (tv.reg[i].x & 0x7f807f80u) + 0x00800080u;
+                bad |= (tv.reg[i].y & 0x7f807f80u) + 0x00800080u;
+                bad |= (tv.reg[i].z & 0x7f807f80u) + 0x00800080u;
+                bad |= (tv.reg[i].w & 0x7f807f80u) + 0x00800080u;
             }
-            if (bad) odd[c & 1] = 1;
+            if (bad & 0x80008000u) odd[c & 1] = 1;
         }
     };
 
+    bf16_t* my_o = o + l32 * a.os.t + 32 * wave + 8 * half;
     const int chunks = (live + C - 1) / C;
     if (chunks) {
         load(0);
@@ -176,14 +195,12 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
                 for (int g = 0; g < 2; ++g) {
                     const int j = 32 * J + 16 * g + 8 * half;
                     float p[8];
-                    bf16x8 hi, lo;
+                    bf16x8 part[2];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) p[e] = i >= j + e ? s[8 * g + e] * power[max(i - j - e, 0)] : 0.f;
-                    split(p, hi, lo);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) lo[e] = finite((float)hi[e]) ? lo[e] : (__bf16)0.f;
-                    *reinterpret_cast<bf16x8*>(sp + i * P_STRIDE + j) = hi;
-                    *reinterpret_cast<bf16x8*>(sp + (C + i) * P_STRIDE + j) = lo;
+                    split<2>(p, part);
+                    *reinterpret_cast<bf16x8*>(sp + i * P_STRIDE + j) = part[0];
+                    *reinterpret_cast<bf16x8*>(sp + (C + i) * P_STRIDE + j) = part[1];
                 }
             }
             // what the state before the chunk gives
@@ -195,15 +212,15 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
 #pragma unroll
                 for (int x = 0; x < 2 * KT; ++x) {
                     float s8[8];
-                    bf16x8 hi, lo;
+                    bf16x8 part[2];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) s8[e] = S[x >> 1][8 * (x & 1) + e];
-                    split(s8, hi, lo);
+                    split<2>(s8, part);
 #pragma unroll
                     for (int I = 0; I < 2; ++I) {
                         const bf16x8 b = read8(sq + (32 * I + l32) * KS + 16 * x + 8 * half);
-                        out[I] = mma(hi, b, out[I]);
-                        out[I] = mma(lo, b, out[I]);
+                        out[I] = mma(part[0], b, out[I]);
+                        out[I] = mma(part[1], b, out[I]);
                     }
                 }
 #pragma unroll
@@ -242,16 +259,16 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
                     }
                 }
                 float wv[8];
-                bf16x8 hi, mid, lo;
+                bf16x8 part[3];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) wv[e] = (float)vv[e] * weight[16 * s + 8 * half + e];
-                split3(wv, hi, mid, lo);
+                split<3>(wv, part);
 #pragma unroll
                 for (int x = 0; x < KT; ++x) {
                     const bf16x8 kk = read_transposed(kt + 16 * s * KS + 32 * x, KS);
-                    S[x] = mma(kk, hi, S[x]);
-                    S[x] = mma(kk, mid, S[x]);
-                    S[x] = mma(kk, lo, S[x]);
+                    S[x] = mma(kk, part[0], S[x]);
+                    S[x] = mma(kk, part[1], S[x]);
+                    S[x] = mma(kk, part[2], S[x]);
                 }
             }
         }
@@ -274,15 +291,14 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
             }
 #pragma unroll
             for (int I = 0; I < 2; ++I) {
-                const int i = 32 * I + l32;
-                bf16_t* row = o + ((int64_t)c * C + i) * a.os.t;
+                bf16_t* row = my_o + ((int64_t)c * C + 32 * I) * a.os.t;
+                const bool there = 32 * I + l32 < n;
 #pragma unroll
                 for (int g = 0; g < 2; ++g) {
-                    const int col = 32 * wave + 16 * g + 8 * half;
                     bf16x8 r;
 #pragma unroll
                     for (int e = 0; e < 8; ++e) r[e] = (__bf16)(a.scale * out[I][8 * g + e]);
-                    if (i < n && col < cols) *reinterpret_cast<bf16x8*>(row + col) = r;
+                    if (there && 32 * wave + 16 * g + 8 * half < cols) *reinterpret_cast<bf16x8*>(row + 16 * g) = r;
                 }
             }
         }

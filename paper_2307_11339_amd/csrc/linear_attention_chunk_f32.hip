@@ -67,41 +67,57 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_f32_kernel(const LaArgs a) {
     if (!STATES && live > 0) from = at.piece > 0 || (a.pieces > 1 && a.s0) ? a.seams + at.piece * states : a.s0;
     if (!STATES && live == 0 && at.piece == 0) from = a.s0;
     f32x16 S[KT];
+    if (from) {
+        // all loads at once, of a place that is there where the state has none
+        const float* col = from + state_at - first_row * (int64_t)a.Dv + (my_col < cols ? 0 : -my_col);
 #pragma unroll
-    for (int x = 0; x < KT; ++x)
+        for (int x = 0; x < KT; ++x)
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-            const int row = 32 * x + 8 * (e >> 2) + (e & 3);
-            S[x][e] = 0.f;
-            if (from && my_col < cols && first_row + row < a.Dk) S[x][e] = from[state_at + (int64_t)row * a.Dv];
-        }
+            for (int e = 0; e < 16; ++e) S[x][e] = col[(int64_t)min(first_row + 32 * x + 8 * (e >> 2) + (e & 3), a.Dk - 1) * a.Dv];
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[x][e] = my_col < cols && first_row + 32 * x + 8 * (e >> 2) + (e & 3) < a.Dk ? S[x][e] : 0.f;
+    } else {
+#pragma unroll
+        for (int x = 0; x < KT; ++x)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) S[x][e] = 0.f;
+    }
 
     KeyTile tq, tk;
     ValueTile tv;
+    if (!STATES) tq.init(q, a.Dk);
+    tk.init(k, a.Dk);
+    tv.init(v, cols);
     auto load = [&](int c) {
         const int n = min(C, live - c * C);
-        if (!STATES) tq.load(q + (int64_t)c * C * a.qs.t, a.qs.t, n, a.Dk);
-        tk.load(k + (int64_t)c * C * a.ks.t, a.ks.t, n, a.Dk);
-        tv.load(v + (int64_t)c * C * a.vs.t, a.vs.t, n, cols);
+        if (!STATES) tq.load((int64_t)c * C * a.qs.t, a.qs.t, n);
+        tk.load((int64_t)c * C * a.ks.t, a.ks.t, n);
+        tv.load((int64_t)c * C * a.vs.t, a.vs.t, n);
     };
     auto store = [&](int c) {
         const int n = min(C, live - c * C);
-        if (!STATES) tq.store(sq);
-        tk.store(sk);
-        tv.store(sv);
-        if (tid < C) weight[tid] = tid < n ? power[n - 1 - tid] : 0.f;
+        if (!STATES) tq.store(sq, n);
+        tk.store(sk, n);
+        tv.store(sv, n);
+        if (c == 0 || n < C) {
+            if (tid < C) weight[tid] = tid < n ? power[n - 1 - tid] : 0.f;
+        }
         if (!STATES) {
-            uint32_t bad = 0;
+            uint32_t bad = 0;          // an exponent of ones carries into the sign
 #pragma unroll
             for (int i = 0; i < ValueTile::N; ++i) {
-                const uint32_t u[4] = {tv.reg[i].x, tv.reg[i].y, tv.reg[i].z, tv.reg[i].w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) bad |= (uint32_t)((u[j] & 0x7f800000u) == 0x7f800000u);
+                bad |= (tv.reg[i].x & 0x7f800000u) + 0x00800000u;
+                bad |= (tv.reg[i].y & 0x7f800000u) + 0x00800000u;
+                bad |= (tv.reg[i].z & 0x7f800000u) + 0x00800000u;
+                bad |= (tv.reg[i].w & 0x7f800000u) + 0x00800000u;
             }
-            if (bad) odd[c & 1] = 1;
+            if (bad & 0x80000000u) odd[c & 1] = 1;
         }
     };
 
+    float* my_o = o + l32 * a.os.t + 32 * wave + 4 * half;
     const int chunks = (live + C - 1) / C;
     if (chunks) {
         load(0);
@@ -193,14 +209,13 @@ __global__ __launch_bounds__(64 * NW) void la_chunk_f32_kernel(const LaArgs a) {
                         if (j <= l32 && !finite(x)) out[e] += sp[l32 * P_STRIDE + j] * x;
                     }
             }
-            float* row = o + ((int64_t)c * C + l32) * a.os.t;
+            float* row = my_o + (int64_t)c * C * a.os.t;
 #pragma unroll
             for (int g = 0; g < 4; ++g) {
-                const int col = 32 * wave + 8 * g + 4 * half;
                 f32x4 r;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) r[e] = a.scale * out[4 * g + e];
-                if (l32 < n && col < cols) *reinterpret_cast<f32x4*>(row + col) = r;
+                if (l32 < n && 32 * wave + 8 * g + 4 * half < cols) *reinterpret_cast<f32x4*>(row + 8 * g) = r;
             }
         }
         __syncthreads();           // the tiles are used up
