@@ -39,14 +39,15 @@ hipError_t la_launch_steps(int dtype, const LaArgs& a, bool wide, hipStream_t st
 hipError_t la_launch_chunks_bf16(const LaArgs& a, int key_tiles, int waves, bool states, hipStream_t stream);
 hipError_t la_launch_chunks_f32(const LaArgs& a, int key_tiles, int waves, bool states, hipStream_t stream);
 
-// Blocks of 32 rows that a chunk kernel holds of a state, and blocks of 32 columns (waves) of a workgroup.
+// Blocks of 32 rows that a chunk kernel holds of a state, and blocks of 16 columns (waves) of a workgroup.  Rows of
+// wide keys are more than few waves can hold on their way to LDS: these have waves without columns.
 inline int la_key_tiles(int Dk) {
     const int t = (Dk + 31) / 32;
     return t <= 4 ? t : t <= 6 ? 6 : 8;
 }
 inline int la_waves(int Dk, int Dv) {
-    const int t = (Dv + 31) / 32, blocks = (t + 3) / 4, w = (t + blocks - 1) / blocks;
-    return Dk > 128 ? 4 : w < 2 ? 2 : w;       // rows of wide keys are more than few waves can hold in flight
+    const int t = (Dv + 15) / 16, blocks = (t + 7) / 8, w = ((t + blocks - 1) / blocks + 1) / 2 * 2;
+    return Dk > 128 ? 8 : Dk > 64 && w < 4 ? 4 : w;
 }
 
 // Where a workgroup of a chunk kernel works.  Workgroups go to the eight XCDs in turn: those that read the same keys
@@ -78,47 +79,60 @@ inline int64_t la_grid(const LaArgs& a, int pieces) {
     return (units + 7) / 8 * 8 * a.rep * a.vblocks;
 }
 
-// The rows [0, n) of a [ROWS, WIDTH] tile on their way from memory to LDS, N pieces of 16 bytes a thread, zeros behind row n
-// and column `width`.  A thread's pieces stand in one column, AT_ONCE rows apart: one address, and scalar offsets to it.
-// Every thread loads, what is not there from a place that is, and the zeros are put in on the way to LDS: a load under a
-// condition would make the wave wait for it at once, where the two ways meet.
+// Tiles in LDS: rows of ROW bytes (64, 128, 256 or 512), whose pieces of 16 bytes change places from row to row, so that
+// both ways of reading a tile find their pieces in different banks: one piece of each of 16 rows (an operand whose index
+// of the sum runs along the row), and four neighbouring pieces of each of four rows (a transposed read).
+template <int ROW>
+__device__ inline int la_turn(int row) {
+    return ROW >= 256 ? (row & 3) << 2 | (row >> 2 & 3) : ROW == 128 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : row >> 2 & 3;
+}
+template <int ROW>
+__device__ inline int la_piece(int row, int piece) { return row * ROW + ((piece ^ la_turn<ROW>(row)) << 4); }
+
+// Block `block` of 64 bytes (four pieces) of the row whose piece 0..3 stands at `at`: the turn of a row reaches two bits of it.
+__device__ inline int la_block(int at, int block) { return (at ^ ((block & 3) << 6)) + ((block >> 2) << 8); }
+
+// A number that the compiler takes for new: what is computed from it is computed here, not kept in registers over a loop.
+__device__ inline int la_fresh(int x) {
+    asm volatile("" : "+v"(x));
+    return x;
+}
+
+constexpr int la_row_bytes(int bytes) { return bytes <= 64 ? 64 : bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : 1024; }
+
+typedef __attribute__((ext_vector_type(4))) uint32_t la_u32x4;
+
+// A tile of ROWS rows of WIDTH elements on its way from memory to LDS, N pieces of 16 bytes a thread.  The loads are bounded
+// by the buffer they are given, the live rows of a chunk: what lies behind is read as zero, without a condition in the code.
 template <typename T, int ROWS, int WIDTH, int THREADS>
 struct LaTile {
-    static constexpr int VEC = 16 / sizeof(T);
+    static constexpr int VEC = 16 / sizeof(T), ROW = la_row_bytes(WIDTH * sizeof(T));
     static constexpr int PER_ROW = WIDTH / VEC, AT_ONCE = THREADS / PER_ROW, N = (ROWS + AT_ONCE - 1) / AT_ONCE;
-    static constexpr int STRIDE = WIDTH + VEC;         // of a row in LDS: 16 bytes more, so that rows start in other banks
-    uint4 reg[N];
-    const T* from;
-    int row, at;                                       // of the first piece: its row, its place in LDS
-    bool spare, beyond, part;                          // threads and columns that the tile does not have, whether there are such columns
-    __device__ inline void init(const T* base, int width) {
-        const int c = threadIdx.x % PER_ROW * VEC;
+    static constexpr int BYTES = ROWS * ROW;
+    la_u32x4 reg[N];
+    uint32_t offset;                 // of the first piece
+    int row, piece;
+    // stride: bytes between rows, at least those of `width` elements and at most 2^25: 64 rows end before 2^31, and what is to
+    // be zero is read from there on
+    __device__ inline void init(uint32_t stride, int width) {
         row = threadIdx.x / PER_ROW;
-        spare = THREADS % PER_ROW && row >= AT_ONCE;
-        if (spare) row = 0;
-        beyond = c >= width;
-        part = width < WIDTH;
-        at = row * STRIDE + c;
-        from = base + (beyond ? 0 : c);
+        piece = threadIdx.x % PER_ROW;
+        offset = row < AT_ONCE && piece * VEC < width ? (uint32_t)row * stride + piece * 16 : 0x80000000u;
     }
-    // offset: of the tile's first row; n >= 1
-    __device__ inline void load(int64_t offset, int64_t stride, int n) {
+    // n >= 1 rows from `from` on, the same for all threads
+    __device__ inline void load(const T* from, uint32_t stride, int width, int n) {
+        const __amdgpu_buffer_rsrc_t rows =
+            __builtin_amdgcn_make_buffer_rsrc((void*)from, (short)0, (int)((uint32_t)(min(n, ROWS) - 1) * stride + width * (int)sizeof(T)), 0x00027000);
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            const int r = min(row + i * AT_ONCE, n - 1);
-            reg[i] = *reinterpret_cast<const uint4*>(from + offset + r * stride);
-        }
+        for (int i = 0; i < N; ++i) reg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, offset + i * AT_ONCE * stride, 0, 0);
     }
-    __device__ inline void store(T* lds, int n) {
-        if (n < ROWS || part) {
+    __device__ inline void store(char* lds) const {
+        const int row = la_fresh(this->row), piece = la_fresh(this->piece);
+        if (THREADS % PER_ROW == 0 || row < AT_ONCE) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                if (beyond || row + i * AT_ONCE >= n) reg[i] = make_uint4(0, 0, 0, 0);
-        }
-        if (!spare) {
-#pragma unroll
-            for (int i = 0; i < N; ++i)
-                if ((i + 1) * AT_ONCE <= ROWS || row + i * AT_ONCE < ROWS) *reinterpret_cast<uint4*>(lds + at + i * AT_ONCE * STRIDE) = reg[i];
+                if ((i + 1) * AT_ONCE <= ROWS || row + i * AT_ONCE < ROWS)
+                    *reinterpret_cast<la_u32x4*>(lds + la_piece<ROW>(row + i * AT_ONCE, piece)) = reg[i];
         }
     }
 };

@@ -203,17 +203,21 @@ struct LaPlan {
     bool wide = false;
 };
 
-LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
-    (void)dtype;
+LaPlan steps_plan(int H, int Dv, int T, int B) {
     LaPlan p;
     p.piece_steps = T;
-    if (T < LA_FEWEST_STEPS) {
-        p.wide = (int64_t)B * H * ((Dv + 127) / 128) >= 512;
-        p.vblocks = p.wide ? (Dv + 127) / 128 : (Dv + 31) / 32;
-        return p;
-    }
+    p.wide = (int64_t)B * H * ((Dv + 127) / 128) >= 512;
+    p.vblocks = p.wide ? (Dv + 127) / 128 : (Dv + 31) / 32;
+    return p;
+}
+
+LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
+    (void)dtype;
+    if (T < LA_FEWEST_STEPS) return steps_plan(H, Dv, T, B);
+    LaPlan p;
+    p.piece_steps = T;
     p.chunk = LA_CHUNK;
-    const int cols = 32 * la_waves(Dk, Dv);
+    const int cols = 16 * la_waves(Dk, Dv);
     p.vblocks = (Dv + cols - 1) / cols;
     const int64_t units = (int64_t)B * H * p.vblocks;
     const int64_t want = LA_WORKGROUPS / units, most = T / LA_PIECE_STEPS;
@@ -229,7 +233,7 @@ LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
 
 // Bytes of the seams of any shape: pieces are cut only while B * H * vblocks * pieces stays within LA_WORKGROUPS.
 size_t seam_bytes(int Dk, int Dv) {
-    const int cols = 32 * la_waves(Dk, Dv);
+    const int cols = 16 * la_waves(Dk, Dv);
     return (size_t)(LA_WORKGROUPS / ((Dv + cols - 1) / cols)) * Dk * Dv * sizeof(float);
 }
 
@@ -260,6 +264,12 @@ bool view(const int64_t* strides, int T, int B, int heads, int size, int step, L
     if (w.t > most / T || w.b > most / B || w.h > most / heads) return false;
     *out = w;
     return true;
+}
+
+// Whether the rows of a chunk can be read through one buffer: they follow one another without overlapping, and their offsets
+// stay below 2^31 bytes.  (A tensor repeated along time, or with 32 MiB from step to step, goes one step after the other.)
+bool chunk_rows(const LaView& w, int T, int size, int dtype) {
+    return T == 1 || (w.t >= size && w.t * (dtype == RNN_BF16 ? 2 : 4) < (int64_t)1 << 25);
 }
 
 // Whether no two rows of an output share an element: each dimension, in the order of strides, steps over what those
@@ -390,7 +400,7 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
     if (!l || !q || !k || !v || !o || T < 1 || B < 1) return RNN_EINVAL;
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o | (uintptr_t)s0 | (uintptr_t)sT) & 15) return RNN_EINVAL;
     if ((uintptr_t)lengths & 3) return RNN_EINVAL;
-    const LaPlan p = choose(l->H, l->Dk, l->Dv, l->dtype, T, B);
+    LaPlan p = choose(l->H, l->Dk, l->Dv, l->dtype, T, B);
     const int rc = check_call(l->H, T, B, p);
     if (rc != RNN_OK) return rc;
     const int step = l->dtype == RNN_BF16 ? 8 : 4;
@@ -399,6 +409,8 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
         !view(v_strides, T, B, l->Hkv, l->Dv, step, &a.vs) || !view(o_strides, T, B, l->H, l->Dv, step, &a.os) ||
         !rows_apart(a.os, T, B, l->H, l->Dv))
         return RNN_EINVAL;
+    if (p.chunk && !(chunk_rows(a.qs, T, l->Dk, l->dtype) && chunk_rows(a.ks, T, l->Dk, l->dtype) && chunk_rows(a.vs, T, l->Dv, l->dtype)))
+        p = steps_plan(l->H, l->Dv, T, B);
     int device = -1;
     if (hipGetDevice(&device) != hipSuccess) {
         (void)hipGetLastError();

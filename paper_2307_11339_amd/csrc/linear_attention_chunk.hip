@@ -3,16 +3,20 @@
 // From the state S before a chunk, for step i of it (0 <= i < n, n live steps):
 //   o_i = scale ( decay^(i+1) S^T q_i + sum_{j <= i} decay^(i-j) (q_i . k_j) v_j )
 //   S'  = decay^n S + sum_j k_j (decay^(n-1-j) v_j)^T
-// Each wave owns 32 columns of S and of o, S in its accumulators (fp32) from the first chunk to the last; only the scores
-// pass between waves, through LDS.  All products are 32 x 32 x 16 bf16 matrix instructions with fp32 sums.  What is
+// Each wave owns 16 columns of S and of o, S in its accumulators (fp32) from the first chunk to the last; only the scores
+// pass between waves, through LDS.  All products are 16 x 16 x 32 bf16 matrix instructions with fp32 sums.  What is
 // no bf16 number by itself is handed over as several of them, each the rounded rest of those before: scores times powers of
 // the decay, and the state as an operand, as two (16 bits, far below the rounding of the bf16 output); weighted values as three
 // (24 bits: the state is an fp32 result).
 //
-// Operand layouts.  Of a 32 x 32 result, a lane holds column l % 32 and rows 8 (e / 4) + 4 (l / 32) + e % 4; as an
-// operand of the next product it has to hold eight neighbouring indices of the sum, 8 (l / 32) + 0..7.  So the rows of a
-// left operand are taken in the order row_order(), with which the two agree: the state goes from accumulator to
-// operand without leaving its lane, scores and outputs are written 16 bytes at a time.
+// Operand layouts.  Of a 16 x 16 result, lane l holds column l % 16 and rows 4 (l / 16) + 0..3; as an operand of the next
+// product it has to hold eight neighbouring indices of a sum of 32, 8 (l / 16) + 0..7.  So a pair of results of the state
+// takes its rows in such an order that the two agree: row 4 g + e of result p of the pair is row 8 g + 4 p + e of the 32,
+// and the state goes from accumulator to operand without leaving its lane.
+//
+// What bounds it: one chunk of 128 x 128 takes a workgroup 100 matrix instructions a wave (3200 cycles a SIMD with two
+// workgroups on a compute unit) and about as long in vector instructions (splitting into bf16 numbers) beside 64 KB of
+// memory traffic.
 #include "common.h"
 #include "linear_attention.h"
 
@@ -21,30 +25,24 @@ namespace {
 
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 constexpr int C = LA_CHUNK;
-constexpr int P_STRIDE = C + 8;
+constexpr int P_ROW = 2 * C;          // bytes of a row of scores
 
-// The index that row r of a left operand stands for: element e of half h of the result then stands for 16 (e / 8) + 8 h + e % 8.
-__device__ inline int row_order(int r) {
-    const int h = (r >> 2) & 1, e = (r >> 3) * 4 + (r & 3);
-    return (e >> 3) * 16 + h * 8 + (e & 7);
-}
-
-__device__ inline f32x16 mma(bf16x8 a, bf16x8 b, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+__device__ inline f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 __device__ inline bool finite(float x) { return fabsf(x) < __builtin_inff(); }
 
-__device__ inline bf16x8 read8(const bf16_t* p) { return *reinterpret_cast<const bf16x8*>(p); }
+__device__ inline bf16x8 read8(const char* p) { return *reinterpret_cast<const bf16x8*>(p); }
 
-// Eight rows j, j + 1, .. of one column each, from a row-major tile: `at` is the lane's own piece, row j + (l % 16) / 4 of
-// the four columns of its group that stand at l % 4; four rows each time.
-__device__ inline bf16x8 read_transposed(const bf16_t* at, int stride) {
-    const bf16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)at);
-    const bf16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)(at + 4 * stride));
-    return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
+// Eight rows of one column each, from a row-major tile: a and b are the lane's own pieces, in row (l % 16) / 4 of the first
+// and of the last four rows, of the four columns that stand at l % 4 among the group's sixteen.
+__device__ inline bf16x8 read_transposed(const char* a, const char* b) {
+    const bf16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)a);
+    const bf16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_bf16x4*)b);
+    return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // Two numbers rounded to bf16 (nearest, even) in one word, and what the rounding took.
@@ -73,16 +71,16 @@ __device__ inline void split(const float* x, bf16x8 (&part)[PARTS]) {
 }
 
 template <int KT, int NW, bool STATES>
-__global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(const LaArgs a) {
-    constexpr int DK = 32 * KT, DV = 32 * NW, THREADS = 64 * NW;
+__global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(const LaArgs a) {
+    constexpr int DK = 32 * KT, DV = 16 * NW, THREADS = 64 * NW;
     typedef LaTile<bf16_t, C, DK, THREADS> KeyTile;
     typedef LaTile<bf16_t, C, DV, THREADS> ValueTile;
-    constexpr int KS = KeyTile::STRIDE, VS = ValueTile::STRIDE;
-    __shared__ __attribute__((aligned(16))) bf16_t sq[STATES ? 8 : C * KS];
-    __shared__ __attribute__((aligned(16))) bf16_t sk[C * KS];
-    __shared__ __attribute__((aligned(16))) bf16_t sv[C * VS];
-    __shared__ __attribute__((aligned(16))) bf16_t sp[STATES ? 8 : 2 * C * P_STRIDE];     // scores: rounded, rest
-    __shared__ __attribute__((aligned(16))) float power[C + 4], weight[C];
+    constexpr int KR = KeyTile::ROW, VR = ValueTile::ROW;
+    __shared__ __attribute__((aligned(1024))) char sq[STATES ? 16 : KeyTile::BYTES];
+    __shared__ __attribute__((aligned(1024))) char sk[KeyTile::BYTES];
+    __shared__ __attribute__((aligned(1024))) char sv[ValueTile::BYTES];
+    __shared__ __attribute__((aligned(1024))) char sp[STATES ? 16 : 2 * C * P_ROW];       // scores [i][j]: rounded, rest
+    __shared__ __attribute__((aligned(16))) float power[C + 4], scaled[C + 4], weight[C];
     __shared__ int odd[2];            // whether the values of the chunk (even, odd ones in turn) hold one that is not finite
 
     LaPlace at;
@@ -90,161 +88,158 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
     if (!la_place(a, pieces, DV, &at)) return;
     if (STATES && at.len <= at.t1) return;         // nothing live behind this piece: nobody asks for its state
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-    const int half = lane >> 5, l32 = lane & 31, l16 = lane & 15;
+    const int l16 = lane & 15, g = lane >> 4;
     const int live = min(max(at.len - at.t0, 0), at.t1 - at.t0);
     const int cols = min(DV, a.Dv - at.v0);
-    const bool mine = 32 * wave < cols;            // the last waves of the last block of columns may have none
+    const bool mine = 16 * wave < cols;            // the last waves of the last block of columns may have none
 
     const bf16_t* q = (const bf16_t*)a.q + at.b * a.qs.b + at.h * a.qs.h + at.t0 * a.qs.t;
     const bf16_t* k = (const bf16_t*)a.k + at.b * a.ks.b + at.hk * a.ks.h + at.t0 * a.ks.t;
     const bf16_t* v = (const bf16_t*)a.v + at.b * a.vs.b + at.hk * a.vs.h + at.t0 * a.vs.t + at.v0;
     bf16_t* o = (bf16_t*)a.o + at.b * a.os.b + at.h * a.os.h + at.t0 * a.os.t + at.v0;
 
-    if (tid <= C) power[tid] = a.powers[at.h * (C + 1) + tid];
-    if (THREADS < C + 1 && tid == 0) power[C] = a.powers[at.h * (C + 1) + C];
-    if (tid < 2) odd[tid] = 0;
-    __syncthreads();
-
-    // state: accumulator e of tile x = row 32 x + 16 (e / 8) + 8 half + e % 8, column order(l % 32) of the wave's 32
-    const int my_col = 32 * wave + row_order(l32);
-    const int first_row = 8 * half;
-    const int64_t state_at = (((int64_t)at.b * a.H + at.h) * a.Dk + first_row) * a.Dv + at.v0 + my_col;
-    const int64_t states = (int64_t)a.B * a.H * a.Dk * a.Dv;
-    const float* from = nullptr;
-    if (!STATES && live > 0) from = at.piece > 0 || (a.pieces > 1 && a.s0) ? a.seams + at.piece * states : a.s0;
-    if (!STATES && live == 0 && at.piece == 0) from = a.s0;
-    f32x16 S[KT];
-    if (from) {
-        // all loads at once, of a place that is there where the state has none
-        const float* col = from + state_at - first_row * (int64_t)a.Dv + (my_col < cols ? 0 : -my_col);
-#pragma unroll
-        for (int x = 0; x < KT; ++x)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) S[x][e] = col[(int64_t)min(first_row + 32 * x + 16 * (e >> 3) + (e & 7), a.Dk - 1) * a.Dv];
-#pragma unroll
-        for (int x = 0; x < KT; ++x)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) S[x][e] = my_col < cols && first_row + 32 * x + 16 * (e >> 3) + (e & 7) < a.Dk ? S[x][e] : 0.f;
-    } else {
-#pragma unroll
-        for (int x = 0; x < KT; ++x)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) S[x][e] = 0.f;
-    }
-
     KeyTile tq, tk;
     ValueTile tv;
-    if (!STATES) tq.init(q, a.Dk);
-    tk.init(k, a.Dk);
-    tv.init(v, cols);
+    if (!STATES) tq.init((uint32_t)a.qs.t * 2, a.Dk);
+    tk.init((uint32_t)a.ks.t * 2, a.Dk);
+    tv.init((uint32_t)a.vs.t * 2, cols);
     auto load = [&](int c) {
-        const int n = min(C, live - c * C);
-        if (!STATES) tq.load((int64_t)c * C * a.qs.t, a.qs.t, n);
-        tk.load((int64_t)c * C * a.ks.t, a.ks.t, n);
-        tv.load((int64_t)c * C * a.vs.t, a.vs.t, n);
+        const int n = live - c * C;
+        if (!STATES) tq.load(q + (int64_t)c * C * a.qs.t, (uint32_t)a.qs.t * 2, a.Dk, n);
+        tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 2, a.Dk, n);
+        tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 2, cols, n);
     };
     auto store = [&](int c) {
         const int n = min(C, live - c * C);
-        if (!STATES) tq.store(sq, n);
-        tk.store(sk, n);
-        tv.store(sv, n);
+        if (!STATES) tq.store(sq);
+        tk.store(sk);
+        tv.store(sv);
         if (c == 0 || n < C) {
             if (tid < C) weight[tid] = tid < n ? power[n - 1 - tid] : 0.f;
         }
         if (!STATES) {
             uint32_t bad = 0;          // an exponent of ones carries into the sign
 #pragma unroll
-            for (int i = 0; i < ValueTile::N; ++i) {
-                bad |= (tv.reg[i].x & 0x7f807f80u) + 0x00800080u;
-                bad |= (tv.reg[i].y & 0x7f807f80u) + 0x00800080u;
-                bad |= (tv.reg[i].z & 0x7f807f80u) + 0x00800080u;
-                bad |= (tv.reg[i].w & 0x7f807f80u) + 0x00800080u;
-            }
+            for (int i = 0; i < ValueTile::N; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) bad |= (tv.reg[i][j] & 0x7f807f80u) + 0x00800080u;
             if (bad & 0x80008000u) odd[c & 1] = 1;
         }
     };
-
-    bf16_t* my_o = o + l32 * a.os.t + 32 * wave + 8 * half;
     const int chunks = (live + C - 1) / C;
-    if (chunks) {
-        load(0);
-        store(0);
+    if (chunks) load(0);
+
+    for (int i = tid; i <= C; i += THREADS) {
+        const float p = a.powers[at.h * (C + 1) + i];
+        power[i] = p;
+        scaled[i] = p * a.scale;
+    }
+    if (tid < 2) odd[tid] = 0;
+    if (!STATES) {
+        // the blocks of scores behind the diagonal that take part in products of 32 steps: rows 0, columns 1 and 2, 3 of 16
+        for (int i = tid; i < 2 * 2 * 16 * 2; i += THREADS) {
+            const int piece = i & 1, row = i >> 1 & 15, block = i >> 5 & 1, part = i >> 6;
+            *reinterpret_cast<la_u32x4*>(sp + part * C * P_ROW + la_piece<P_ROW>(32 * block + row, 4 * block + 2 + piece)) = la_u32x4{0, 0, 0, 0};
+        }
+    }
+
+    // state: element e of result 2 x + p = row 32 x + 8 g + 4 p + e, column l % 16 of the wave's
+    const int my_col = 16 * wave + l16;
+    const int64_t state_at = ((int64_t)at.b * a.H + at.h) * a.Dk * a.Dv + at.v0;
+    const int64_t states = (int64_t)a.B * a.H * a.Dk * a.Dv;
+    const float* from = nullptr;
+    if (!STATES && live > 0) from = at.piece > 0 || (a.pieces > 1 && a.s0) ? a.seams + at.piece * states : a.s0;
+    if (!STATES && live == 0 && at.piece == 0) from = a.s0;
+    f32x4 S[2 * KT];
+    if (from) {
+        // all loads at once, of a place that is there where the state has none
+        const float* col = from + state_at + (my_col < cols ? my_col : 0);
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[y][e] = col[min(32 * (y >> 1) + 8 * g + 4 * (y & 1) + e, a.Dk - 1) * a.Dv];
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) S[y][e] = my_col < cols && 32 * (y >> 1) + 8 * g + 4 * (y & 1) + e < a.Dk ? S[y][e] : 0.f;
+    } else {
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y) S[y] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     __syncthreads();
+    if (chunks) store(0);
+    __syncthreads();
+
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
         const int n = min(C, live - c * C);
-        if (c + 1 < chunks) load(c + 1);
-        f32x16 out[2];
+        if (STATES && c + 1 < chunks) load(c + 1);
+        f32x4 out[4];
         bool strange = false;
+        // the lane's places in the tiles; found anew for each chunk: they are cheap, and registers are short
+        const int l16 = la_fresh(lane & 15), g = la_fresh(lane >> 4);
+        const int row_at = la_piece<KR>(l16, g), p_at = la_piece<P_ROW>(l16, g);
+        // transposed: rows 8 g + l16 / 4 and four further, four columns at l16 % 4 (of the state's order, of the wave's own)
+        const int tr = 8 * g + (l16 >> 2), tc = l16 & 3;
+        const int kt_a = la_piece<KR>(tr, tc), kt_b = la_piece<KR>(tr + 4, tc);
+        const char* v_a = sv + la_piece<VR>(tr, 2 * wave + (tc >> 1)) + 8 * (tc & 1);
+        const char* v_b = sv + la_piece<VR>(tr + 4, 2 * wave + (tc >> 1)) + 8 * (tc & 1);
         if (!STATES) {
             strange = __builtin_amdgcn_readfirstlane(odd[c & 1]) != 0;
-            // scores of rows j of block J and columns i of block I; block (1, 0) is behind the diagonal
+            // scores: blocks of 16 rows j and 16 columns i on and below the diagonal
 #pragma unroll 1
-            for (int t = wave; t < 3; t += NW) {
-                const int I = t == 0 ? 0 : 1, J = t == 1 ? 1 : 0;
-                f32x16 s;
+            for (int t = wave; t < 10; t += NW) {
+                const int I = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, J = t - I * (I + 1) / 2;
+                f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[e] = 0.f;
-                const bf16_t* kr = sk + (32 * J + row_order(l32)) * KS + 8 * half;
-                const bf16_t* qr = sq + (32 * I + l32) * KS + 8 * half;
-#pragma unroll
-                for (int x = 0; x < 2 * KT; ++x) s = mma(read8(kr + 16 * x), read8(qr + 16 * x), s);
-                const int i = 32 * I + l32;
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const int j = 32 * J + 16 * g + 8 * half;
-                    float p[8];
-                    bf16x8 part[2];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) p[e] = i >= j + e ? s[8 * g + e] * power[max(i - j - e, 0)] : 0.f;
-                    split<2>(p, part);
-                    *reinterpret_cast<bf16x8*>(sp + i * P_STRIDE + j) = part[0];
-                    *reinterpret_cast<bf16x8*>(sp + (C + i) * P_STRIDE + j) = part[1];
+                for (int x = 0; x < KT; ++x) {
+                    const bf16x8 kk = read8(sk + J * 16 * KR + la_block(row_at, x));
+                    const bf16x8 qq = read8(sq + I * 16 * KR + la_block(row_at, x));
+                    s = mma(kk, qq, s);
                 }
+                const int i = 16 * I + l16, j = 16 * J + 4 * g;
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = i >= j + e ? s[e] * scaled[max(i - j - e, 0)] : 0.f;
+                uint2 hi, lo;
+                hi.x = round2(p[0], p[1]);
+                hi.y = round2(p[2], p[3]);
+                lo.x = round2(p[0], p[1]);
+                lo.y = round2(p[2], p[3]);
+                char* to = sp + la_piece<P_ROW>(i, 2 * J + (g >> 1)) + 8 * (g & 1);
+                *reinterpret_cast<uint2*>(to) = hi;
+                *reinterpret_cast<uint2*>(to + C * P_ROW) = lo;
             }
             // what the state before the chunk gives
             if (mine) {
 #pragma unroll
-                for (int I = 0; I < 2; ++I)
+                for (int I = 0; I < 4; ++I) out[I] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) out[I][e] = 0.f;
+                for (int x = 0; x < KT; ++x) {
+                    const float s8[8] = {S[2 * x][0], S[2 * x][1], S[2 * x][2], S[2 * x][3],
+                                         S[2 * x + 1][0], S[2 * x + 1][1], S[2 * x + 1][2], S[2 * x + 1][3]};
+                    bf16x8 part[2], b[4];
 #pragma unroll
-                for (int x = 0; x < 2 * KT; ++x) {
-                    float s8[8];
-                    bf16x8 part[2];
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) s8[e] = S[x >> 1][8 * (x & 1) + e];
+                    for (int I = 0; I < 4; ++I) b[I] = read8(sq + I * 16 * KR + la_block(row_at, x));
                     split<2>(s8, part);
 #pragma unroll
-                    for (int I = 0; I < 2; ++I) {
-                        const bf16x8 b = read8(sq + (32 * I + l32) * KS + 16 * x + 8 * half);
-                        out[I] = mma(part[0], b, out[I]);
-                        out[I] = mma(part[1], b, out[I]);
-                    }
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int I = 0; I < 4; ++I) out[I] = mma(part[p], b[I], out[I]);
                 }
 #pragma unroll
-                for (int I = 0; I < 2; ++I) {
-                    const float w = power[32 * I + l32 + 1];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) out[I][e] *= w;
-                }
+                for (int I = 0; I < 4; ++I) out[I] *= scaled[16 * I + l16 + 1];
             }
             __syncthreads();       // the scores are there
+            if (c + 1 < chunks) load(c + 1);        // not before: the operands above need the registers
         }
         if (mine) {
             const float w = power[n];
 #pragma unroll
-            for (int x = 0; x < KT; ++x)
+            for (int y = 0; y < 2 * KT; ++y) S[y] *= w;
 #pragma unroll
-                for (int e = 0; e < 16; ++e) S[x][e] *= w;
-            // the lane's piece of a transposed read: row l16 / 4 of its eight, four columns that row_order puts at 4 (l16 % 4)
-            const int quad = row_order(16 * ((lane >> 4) & 1) + 4 * (l16 & 3));
-            const bf16_t* vt = sv + (8 * half + (l16 >> 2)) * VS + 32 * wave + quad;
-            const bf16_t* kt = sk + (8 * half + (l16 >> 2)) * KS + quad;
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const bf16x8 vv = read_transposed(vt + 16 * s * VS, VS);
+            for (int s = 0; s < 2; ++s) {
+                const bf16x8 vv = read_transposed(v_a + 32 * s * VR, v_b + 32 * s * VR);
                 if (!STATES) {
                     bf16x8 clean = vv;
                     if (strange) {
@@ -252,23 +247,26 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
                         for (int e = 0; e < 8; ++e) clean[e] = finite((float)vv[e]) ? vv[e] : (__bf16)0.f;
                     }
 #pragma unroll
-                    for (int I = s / 2; I < 2; ++I) {
-                        const bf16_t* p = sp + (32 * I + l32) * P_STRIDE + 16 * s + 8 * half;
-                        out[I] = mma(clean, read8(p), out[I]);
-                        out[I] = mma(clean, read8(p + C * P_STRIDE), out[I]);
-                    }
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int I = 2 * s; I < 4; ++I)
+                            out[I] = mma(clean, read8(sp + p * C * P_ROW + I * 16 * P_ROW + (p_at ^ (s << 6))), out[I]);
                 }
                 float wv[8];
                 bf16x8 part[3];
 #pragma unroll
-                for (int e = 0; e < 8; ++e) wv[e] = (float)vv[e] * weight[16 * s + 8 * half + e];
+                for (int e = 0; e < 8; ++e) wv[e] = (float)vv[e] * weight[32 * s + 8 * g + e];
                 split<3>(wv, part);
 #pragma unroll
                 for (int x = 0; x < KT; ++x) {
-                    const bf16x8 kk = read_transposed(kt + 16 * s * KS + 32 * x, KS);
-                    S[x] = mma(kk, part[0], S[x]);
-                    S[x] = mma(kk, part[1], S[x]);
-                    S[x] = mma(kk, part[2], S[x]);
+                    bf16x8 kk[2];
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+                        kk[p] = read_transposed(sk + 32 * s * KR + 8 * p + la_block(kt_a, x), sk + 32 * s * KR + 8 * p + la_block(kt_b, x));
+#pragma unroll
+                    for (int j = 0; j < 3; ++j)
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) S[2 * x + p] = mma(kk[p], part[j], S[2 * x + p]);
                 }
             }
         }
@@ -276,30 +274,31 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
             if (strange) {
                 // A value that is not finite, times the zero above the diagonal, would reach steps before its own: such
                 // values were left out of the product and are added here to the steps that they belong to.
-#pragma unroll
-                for (int I = 0; I < 2; ++I) {
-                    const int i = 32 * I + l32;
 #pragma unroll 1
-                    for (int j = 0; j < C; ++j)
+                for (int j = 0; j < C; ++j) {
+                    const char* vx = sv + la_piece<VR>(j, 2 * wave + (g >> 1)) + 8 * (g & 1);
 #pragma unroll
-                        for (int e = 0; e < 16; ++e) {
-                            const float x = bf16_to_f32(sv[j * VS + 32 * wave + 16 * (e >> 3) + 8 * half + (e & 7)]);
-                            if (j <= i && !finite(x))
-                                out[I][e] += (bf16_to_f32(sp[i * P_STRIDE + j]) + bf16_to_f32(sp[(C + i) * P_STRIDE + j])) * x;
+                    for (int I = 0; I < 4; ++I) {
+                        const int i = 16 * I + l16;
+                        const char* px = sp + la_piece<P_ROW>(i, j >> 3) + 2 * (j & 7);
+                        const float p = bf16_to_f32(*(const bf16_t*)px) + bf16_to_f32(*(const bf16_t*)(px + C * P_ROW));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            const float x = bf16_to_f32(((const bf16_t*)vx)[e]);
+                            if (j <= i && !finite(x)) out[I][e] += p * x;
                         }
+                    }
                 }
             }
+            bf16_t* my_o = o + ((int64_t)c * C + l16) * a.os.t + 16 * wave + 4 * g;
 #pragma unroll
-            for (int I = 0; I < 2; ++I) {
-                bf16_t* row = my_o + ((int64_t)c * C + 32 * I) * a.os.t;
-                const bool there = 32 * I + l32 < n;
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    bf16x8 r;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) r[e] = (__bf16)(a.scale * out[I][8 * g + e]);
-                    if (there && 32 * wave + 16 * g + 8 * half < cols) *reinterpret_cast<bf16x8*>(row + 16 * g) = r;
-                }
+            for (int I = 0; I < 4; ++I) {
+                float r[4] = {out[I][0], out[I][1], out[I][2], out[I][3]};
+                uint2 w;
+                w.x = round2(r[0], r[1]);
+                w.y = round2(r[2], r[3]);
+                if (16 * I + l16 < n && 16 * wave + 4 * g < cols)
+                    *reinterpret_cast<uint2*>(my_o + 16 * I * a.os.t) = w;
             }
         }
         __syncthreads();           // the tiles are used up
@@ -315,11 +314,11 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 2 : 1) void la_chunk_kernel(cons
     asm volatile("" : "+s"(dv));
     auto write_state = [&](float* to) {
 #pragma unroll
-        for (int x = 0; x < KT; ++x)
+        for (int y = 0; y < 2 * KT; ++y)
 #pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                const int row = 32 * x + 16 * (e >> 3) + (e & 7);
-                if (my_col < cols && first_row + row < a.Dk) to[state_at + (int64_t)row * dv] = S[x][e];
+            for (int e = 0; e < 4; ++e) {
+                const int row = 32 * (y >> 1) + 8 * g + 4 * (y & 1) + e;
+                if (my_col < cols && row < a.Dk) to[state_at + row * dv + my_col] = S[y][e];
             }
     };
     if (STATES) {
@@ -338,11 +337,11 @@ bool launch(const LaArgs& a, int kt, int nw, hipStream_t stream) {
     const unsigned grid = (unsigned)la_grid(a, STATES ? a.pieces - 1 : a.pieces);
 #define LA_CHUNK_CASE(K, N) \
     if (kt == K && nw == N) { la_chunk_kernel<K, N, STATES><<<grid, 64 * N, 0, stream>>>(a); return true; }
-    LA_CHUNK_CASE(1, 2) LA_CHUNK_CASE(1, 3) LA_CHUNK_CASE(1, 4)
-    LA_CHUNK_CASE(2, 2) LA_CHUNK_CASE(2, 3) LA_CHUNK_CASE(2, 4)
-    LA_CHUNK_CASE(3, 2) LA_CHUNK_CASE(3, 3) LA_CHUNK_CASE(3, 4)
-    LA_CHUNK_CASE(4, 2) LA_CHUNK_CASE(4, 3) LA_CHUNK_CASE(4, 4)
-    LA_CHUNK_CASE(6, 4) LA_CHUNK_CASE(8, 4)
+    LA_CHUNK_CASE(1, 2) LA_CHUNK_CASE(1, 4) LA_CHUNK_CASE(1, 6) LA_CHUNK_CASE(1, 8)
+    LA_CHUNK_CASE(2, 2) LA_CHUNK_CASE(2, 4) LA_CHUNK_CASE(2, 6) LA_CHUNK_CASE(2, 8)
+    LA_CHUNK_CASE(3, 4) LA_CHUNK_CASE(3, 6) LA_CHUNK_CASE(3, 8)
+    LA_CHUNK_CASE(4, 4) LA_CHUNK_CASE(4, 6) LA_CHUNK_CASE(4, 8)
+    LA_CHUNK_CASE(6, 8) LA_CHUNK_CASE(8, 8)
 #undef LA_CHUNK_CASE
     return false;
 }
