@@ -79,12 +79,15 @@ inline int64_t la_grid(const LaArgs& a, int pieces) {
     return (units + 7) / 8 * 8 * a.rep * a.vblocks;
 }
 
-// Tiles in LDS: rows of ROW bytes (64, 128, 256 or 512), whose pieces of 16 bytes change places from row to row, so that
-// both ways of reading a tile find their pieces in different banks: one piece of each of 16 rows (an operand whose index
-// of the sum runs along the row), and four neighbouring pieces of each of four rows (a transposed read).
+// Tiles in LDS: rows of ROW bytes (64 to 1024), whose pieces of 16 bytes change places from row to row, so that the ways of
+// reading a tile find their pieces in different banks: one piece of each of 16 rows (an operand whose index of the sum
+// runs along the row; 4 cycles a wave, 8 where two rows meet) and two neighbouring pieces of each of 16 rows (a transposed
+// read; 2 cycles).  Found by measuring all ways to add bits of the row to those of the piece.
 template <int ROW>
 __device__ inline int la_turn(int row) {
-    return ROW >= 256 ? (row & 3) << 2 | (row >> 2 & 3) : ROW == 128 ? (row >> 1 & 1) << 2 | (row >> 2 & 3) : row >> 2 & 3;
+    if (ROW >= 256) return ((row & 3) << 2 | (row >> 2 & 3)) ^ (row >> 1 & 2);
+    if (ROW == 128) return (row & 1) | (row >> 2 & 2) | (row & 2) << 1;
+    return row >> 2 & 3;
 }
 template <int ROW>
 __device__ inline int la_piece(int row, int piece) { return row * ROW + ((piece ^ la_turn<ROW>(row)) << 4); }
