@@ -95,6 +95,10 @@ __device__ inline int la_piece(int row, int piece) { return row * ROW + ((piece 
 // Block `block` of 64 bytes (four pieces) of the row whose piece 0..3 stands at `at`: the turn of a row reaches two bits of it.
 __device__ inline int la_block(int at, int block) { return (at ^ ((block & 3) << 6)) + ((block >> 2) << 8); }
 
+// The decay of a chunk is kept out of the state, as a factor `gain` of it, while that is no smaller than this: the state is
+// multiplied by it now and then and not with every chunk.
+constexpr float LA_LEAST_GAIN = 1.0f / 1024;
+
 // A number that the compiler takes for new: what is computed from it is computed here, not kept in registers over a loop.
 __device__ inline int la_fresh(int x) {
     asm volatile("" : "+v"(x));
@@ -104,6 +108,13 @@ __device__ inline int la_fresh(int x) {
 constexpr int la_row_bytes(int bytes) { return bytes <= 64 ? 64 : bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : 1024; }
 
 typedef __attribute__((ext_vector_type(4))) uint32_t la_u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t la_u32x2;
+
+// n >= 1 rows of `width` elements as a buffer: reads behind them give zero, writes do nothing.
+template <typename T>
+__device__ inline __amdgpu_buffer_rsrc_t la_rows(const T* from, uint32_t stride, int width, int n) {
+    return __builtin_amdgcn_make_buffer_rsrc((void*)from, (short)0, (int)((uint32_t)(n - 1) * stride + width * (int)sizeof(T)), 0x00027000);
+}
 
 // A tile of ROWS rows of WIDTH elements on its way from memory to LDS, N pieces of 16 bytes a thread.  The loads are bounded
 // by the buffer they are given, the live rows of a chunk: what lies behind is read as zero, without a condition in the code.
@@ -114,23 +125,22 @@ struct LaTile {
     static constexpr int BYTES = ROWS * ROW;
     la_u32x4 reg[N];
     uint32_t offset;                 // of the first piece
-    int row, piece;
     // stride: bytes between rows, at least those of `width` elements and at most 2^25: 64 rows end before 2^31, and what is to
     // be zero is read from there on
     __device__ inline void init(uint32_t stride, int width) {
-        row = threadIdx.x / PER_ROW;
-        piece = threadIdx.x % PER_ROW;
+        const int row = threadIdx.x / PER_ROW, piece = threadIdx.x % PER_ROW;
         offset = row < AT_ONCE && piece * VEC < width ? (uint32_t)row * stride + piece * 16 : 0x80000000u;
     }
     // n >= 1 rows from `from` on, the same for all threads
     __device__ inline void load(const T* from, uint32_t stride, int width, int n) {
-        const __amdgpu_buffer_rsrc_t rows =
-            __builtin_amdgcn_make_buffer_rsrc((void*)from, (short)0, (int)((uint32_t)(min(n, ROWS) - 1) * stride + width * (int)sizeof(T)), 0x00027000);
+        const __amdgpu_buffer_rsrc_t rows = la_rows(from, stride, width, min(n, ROWS));
+        const uint32_t first = la_fresh(offset);
 #pragma unroll
-        for (int i = 0; i < N; ++i) reg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, offset + i * AT_ONCE * stride, 0, 0);
+        for (int i = 0; i < N; ++i) reg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, first + i * AT_ONCE * stride, 0, 0);
     }
-    __device__ inline void store(char* lds) const {
-        const int row = la_fresh(this->row), piece = la_fresh(this->piece);
+    // thread: its number, fresh (the place is found anew instead of being kept)
+    __device__ inline void store(char* lds, int thread) const {
+        const int row = thread / PER_ROW, piece = thread % PER_ROW;
         if (THREADS % PER_ROW == 0 || row < AT_ONCE) {
 #pragma unroll
             for (int i = 0; i < N; ++i)

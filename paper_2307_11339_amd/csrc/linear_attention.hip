@@ -409,7 +409,8 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
         !view(v_strides, T, B, l->Hkv, l->Dv, step, &a.vs) || !view(o_strides, T, B, l->H, l->Dv, step, &a.os) ||
         !rows_apart(a.os, T, B, l->H, l->Dv))
         return RNN_EINVAL;
-    if (p.chunk && !(chunk_rows(a.qs, T, l->Dk, l->dtype) && chunk_rows(a.ks, T, l->Dk, l->dtype) && chunk_rows(a.vs, T, l->Dv, l->dtype)))
+    if (p.chunk && !(chunk_rows(a.qs, T, l->Dk, l->dtype) && chunk_rows(a.ks, T, l->Dk, l->dtype) && chunk_rows(a.vs, T, l->Dv, l->dtype) &&
+                     chunk_rows(a.os, T, l->Dv, l->dtype)))
         p = steps_plan(l->H, l->Dv, T, B);
     int device = -1;
     if (hipGetDevice(&device) != hipSuccess) {

@@ -81,7 +81,6 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
     __shared__ __attribute__((aligned(1024))) char sv[ValueTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sp[STATES ? 16 : 2 * C * P_ROW];       // scores [i][j]: rounded, rest
     __shared__ __attribute__((aligned(16))) float power[C + 4], scaled[C + 4], weight[C];
-    __shared__ int odd[2];            // whether the values of the chunk (even, odd ones in turn) hold one that is not finite
 
     LaPlace at;
     const int pieces = STATES ? a.pieces - 1 : a.pieces;
@@ -109,21 +108,15 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
         tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 2, a.Dk, n);
         tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 2, cols, n);
     };
-    auto store = [&](int c) {
-        const int n = min(C, live - c * C);
-        if (!STATES) tq.store(sq);
-        tk.store(sk);
-        tv.store(sv);
-        if (c == 0 || n < C) {
-            if (tid < C) weight[tid] = tid < n ? power[n - 1 - tid] : 0.f;
-        }
-        if (!STATES) {
-            uint32_t bad = 0;          // an exponent of ones carries into the sign
-#pragma unroll
-            for (int i = 0; i < ValueTile::N; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) bad |= (tv.reg[i][j] & 0x7f807f80u) + 0x00800080u;
-            if (bad & 0x80008000u) odd[c & 1] = 1;
+    // gain: of the state before chunk c
+    auto store = [&](int c, float gain) {
+        const int n = min(C, live - c * C), thread = la_fresh(tid);
+        if (!STATES) tq.store(sq, thread);
+        tk.store(sk, thread);
+        tv.store(sv, thread);
+        if (tid < C) {
+            const float next = gain * power[n];
+            weight[tid] = tid < n ? power[n - 1 - tid] * (next < LA_LEAST_GAIN ? 1.f : 1.f / next) : 0.f;
         }
     };
     const int chunks = (live + C - 1) / C;
@@ -134,7 +127,6 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
         power[i] = p;
         scaled[i] = p * a.scale;
     }
-    if (tid < 2) odd[tid] = 0;
     if (!STATES) {
         // the blocks of scores behind the diagonal that take part in products of 32 steps: rows 0, columns 1 and 2, 3 of 16
         for (int i = tid; i < 2 * 2 * 16 * 2; i += THREADS) {
@@ -167,15 +159,15 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
         for (int y = 0; y < 2 * KT; ++y) S[y] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     __syncthreads();
-    if (chunks) store(0);
+    if (chunks) store(0, 1.f);
     __syncthreads();
 
+    float gain = 1.f;             // what S is to be multiplied by
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
         const int n = min(C, live - c * C);
         if (STATES && c + 1 < chunks) load(c + 1);
         f32x4 out[4];
-        bool strange = false;
         // the lane's places in the tiles; found anew for each chunk: they are cheap, and registers are short
         const int l16 = la_fresh(lane & 15), g = la_fresh(lane >> 4);
         const int row_at = la_piece<KR>(l16, g), p_at = la_piece<P_ROW>(l16, g);
@@ -185,7 +177,6 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
         const char* v_a = sv + la_piece<VR>(tr, 2 * wave + (tc >> 1)) + 8 * (tc & 1);
         const char* v_b = sv + la_piece<VR>(tr + 4, 2 * wave + (tc >> 1)) + 8 * (tc & 1);
         if (!STATES) {
-            strange = __builtin_amdgcn_readfirstlane(odd[c & 1]) != 0;
             // scores: blocks of 16 rows j and 16 columns i on and below the diagonal
 #pragma unroll 1
             for (int t = wave; t < 10; t += NW) {
@@ -228,30 +219,21 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
                         for (int I = 0; I < 4; ++I) out[I] = mma(part[p], b[I], out[I]);
                 }
 #pragma unroll
-                for (int I = 0; I < 4; ++I) out[I] *= scaled[16 * I + l16 + 1];
+                for (int I = 0; I < 4; ++I) out[I] *= scaled[16 * I + l16 + 1] * gain;
             }
             __syncthreads();       // the scores are there
             if (c + 1 < chunks) load(c + 1);        // not before: the operands above need the registers
         }
+        gain *= power[n];
+        const bool small = gain < LA_LEAST_GAIN;
         if (mine) {
-            const float w = power[n];
+            if (small) {
 #pragma unroll
-            for (int y = 0; y < 2 * KT; ++y) S[y] *= w;
+                for (int y = 0; y < 2 * KT; ++y) S[y] *= gain;
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
                 const bf16x8 vv = read_transposed(v_a + 32 * s * VR, v_b + 32 * s * VR);
-                if (!STATES) {
-                    bf16x8 clean = vv;
-                    if (strange) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) clean[e] = finite((float)vv[e]) ? vv[e] : (__bf16)0.f;
-                    }
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-#pragma unroll
-                        for (int I = 2 * s; I < 4; ++I)
-                            out[I] = mma(clean, read8(sp + p * C * P_ROW + I * 16 * P_ROW + (p_at ^ (s << 6))), out[I]);
-                }
                 float wv[8];
                 bf16x8 part[3];
 #pragma unroll
@@ -268,44 +250,59 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
 #pragma unroll
                         for (int p = 0; p < 2; ++p) S[2 * x + p] = mma(kk[p], part[j], S[2 * x + p]);
                 }
+                __builtin_amdgcn_sched_barrier(0);      // operands of one half at a time: there are no registers for both
             }
-        }
-        if (!STATES && mine) {
-            if (strange) {
-                // A value that is not finite, times the zero above the diagonal, would reach steps before its own: such
-                // values were left out of the product and are added here to the steps that they belong to.
+            if (!STATES) {
+                // A value that is not finite, times the zero above the diagonal, would reach steps before its own.  It makes
+                // every row of its column of the state not finite: where one is, such values are left out of the product and
+                // added to the steps that they belong to.
+                bf16x8 vv[2];
+#pragma unroll
+                for (int s = 0; s < 2; ++s) vv[s] = read_transposed(v_a + 32 * s * VR, v_b + 32 * s * VR);
+                const bool strange = __builtin_amdgcn_ballot_w64(!finite(S[0][0])) != 0;
+                if (strange) {
 #pragma unroll 1
-                for (int j = 0; j < C; ++j) {
-                    const char* vx = sv + la_piece<VR>(j, 2 * wave + (g >> 1)) + 8 * (g & 1);
+                    for (int j = 0; j < C; ++j) {
+                        const char* vx = sv + la_piece<VR>(j, 2 * wave + (g >> 1)) + 8 * (g & 1);
 #pragma unroll
-                    for (int I = 0; I < 4; ++I) {
-                        const int i = 16 * I + l16;
-                        const char* px = sp + la_piece<P_ROW>(i, j >> 3) + 2 * (j & 7);
-                        const float p = bf16_to_f32(*(const bf16_t*)px) + bf16_to_f32(*(const bf16_t*)(px + C * P_ROW));
+                        for (int I = 0; I < 4; ++I) {
+                            const int i = 16 * I + l16;
+                            const char* px = sp + la_piece<P_ROW>(i, j >> 3) + 2 * (j & 7);
+                            const float p = bf16_to_f32(*(const bf16_t*)px) + bf16_to_f32(*(const bf16_t*)(px + C * P_ROW));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e) {
-                            const float x = bf16_to_f32(((const bf16_t*)vx)[e]);
-                            if (j <= i && !finite(x)) out[I][e] += p * x;
+                            for (int e = 0; e < 4; ++e) {
+                                const float x = bf16_to_f32(((const bf16_t*)vx)[e]);
+                                if (j <= i && !finite(x)) out[I][e] += p * x;
+                            }
                         }
                     }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) vv[s][e] = finite((float)vv[s][e]) ? vv[s][e] : (__bf16)0.f;
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int I = 2 * s; I < 4; ++I)
+                            out[I] = mma(vv[s], read8(sp + p * C * P_ROW + I * 16 * P_ROW + (p_at ^ (s << 6))), out[I]);
+                const __amdgpu_buffer_rsrc_t rows = la_rows(o + (int64_t)c * C * a.os.t, (uint32_t)a.os.t * 2, cols, n);
+                const uint32_t at_o = 16 * wave + 4 * g < cols ? (uint32_t)l16 * (uint32_t)a.os.t * 2 + 32 * wave + 8 * g : 0x80000000u;
+#pragma unroll
+                for (int I = 0; I < 4; ++I) {
+                    float r[4] = {out[I][0], out[I][1], out[I][2], out[I][3]};
+                    la_u32x2 w;
+                    w[0] = round2(r[0], r[1]);
+                    w[1] = round2(r[2], r[3]);
+                    __builtin_amdgcn_raw_buffer_store_b64(w, rows, at_o + 16 * I * (uint32_t)a.os.t * 2, 0, 0);
                 }
             }
-            bf16_t* my_o = o + ((int64_t)c * C + l16) * a.os.t + 16 * wave + 4 * g;
-#pragma unroll
-            for (int I = 0; I < 4; ++I) {
-                float r[4] = {out[I][0], out[I][1], out[I][2], out[I][3]};
-                uint2 w;
-                w.x = round2(r[0], r[1]);
-                w.y = round2(r[2], r[3]);
-                if (16 * I + l16 < n && 16 * wave + 4 * g < cols)
-                    *reinterpret_cast<uint2*>(my_o + 16 * I * a.os.t) = w;
-            }
         }
+        if (small) gain = 1.f;
         __syncthreads();           // the tiles are used up
-        if (c + 1 < chunks) {
-            if (!STATES && tid == 0) odd[c & 1] = 0;
-            store(c + 1);
-        }
+        if (c + 1 < chunks) store(c + 1, gain);
         __syncthreads();
     }
 
@@ -318,7 +315,7 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int row = 32 * (y >> 1) + 8 * g + 4 * (y & 1) + e;
-                if (my_col < cols && row < a.Dk) to[state_at + row * dv + my_col] = S[y][e];
+                if (my_col < cols && row < a.Dk) to[state_at + row * dv + my_col] = gain * S[y][e];
             }
     };
     if (STATES) {

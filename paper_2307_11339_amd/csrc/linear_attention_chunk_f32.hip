@@ -37,7 +37,6 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
     __shared__ __attribute__((aligned(1024))) char sv[ValueTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sp[STATES ? 16 : C * P_ROW];           // scores [i][j]
     __shared__ __attribute__((aligned(16))) float power[C + 4], scaled[C + 4], weight[C];
-    __shared__ int odd[2];            // whether the values of the chunk (even, odd ones in turn) hold one that is not finite
 
     LaPlace at;
     const int pieces = STATES ? a.pieces - 1 : a.pieces;
@@ -65,21 +64,15 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
         tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 4, a.Dk, n);
         tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 4, cols, n);
     };
-    auto store = [&](int c) {
-        const int n = min(C, live - c * C);
-        if (!STATES) tq.store(sq);
-        tk.store(sk);
-        tv.store(sv);
-        if (c == 0 || n < C) {
-            if (tid < C) weight[step_place(tid)] = tid < n ? power[n - 1 - tid] : 0.f;
-        }
-        if (!STATES) {
-            uint32_t bad = 0;          // an exponent of ones carries into the sign
-#pragma unroll
-            for (int i = 0; i < ValueTile::N; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) bad |= (tv.reg[i][j] & 0x7f800000u) + 0x00800000u;
-            if (bad & 0x80000000u) odd[c & 1] = 1;
+    // gain: of the state before chunk c
+    auto store = [&](int c, float gain) {
+        const int n = min(C, live - c * C), thread = la_fresh(tid);
+        if (!STATES) tq.store(sq, thread);
+        tk.store(sk, thread);
+        tv.store(sv, thread);
+        if (tid < C) {
+            const float next = gain * power[n];
+            weight[step_place(tid)] = tid < n ? power[n - 1 - tid] * (next < LA_LEAST_GAIN ? 1.f : 1.f / next) : 0.f;
         }
     };
     const int chunks = (live + C - 1) / C;
@@ -90,7 +83,6 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
         power[i] = p;
         scaled[i] = p * a.scale;
     }
-    if (tid < 2) odd[tid] = 0;
     if (!STATES) {
         // the block of scores behind the diagonal that takes part in products: rows 0..15, steps 16..31
         if (tid < 64) *reinterpret_cast<la_u32x4*>(sp + la_piece<P_ROW>(tid >> 2, 4 + (tid & 3))) = la_u32x4{0, 0, 0, 0};
@@ -120,15 +112,15 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
         for (int y = 0; y < 2 * KT; ++y) S[y] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
     __syncthreads();
-    if (chunks) store(0);
+    if (chunks) store(0, 1.f);
     __syncthreads();
 
+    float gain = 1.f;             // what S is to be multiplied by
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
         const int n = min(C, live - c * C);
         if (STATES && c + 1 < chunks) load(c + 1);
         f32x4 out[2];
-        bool strange = false;
         // the lane's places in the tiles; found anew for each chunk: they are cheap, and registers are short
         const int l16 = la_fresh(lane & 15), g = la_fresh(lane >> 4);
         const int row_at = la_piece<KR>(l16, g), p_at = la_piece<P_ROW>(l16, g);
@@ -140,7 +132,6 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
             v_at[e] = la_piece<VR>(4 * e + g, 4 * wave + (l16 >> 2)) + 4 * (l16 & 3);
         }
         if (!STATES) {
-            strange = __builtin_amdgcn_readfirstlane(odd[c & 1]) != 0;
             // scores: blocks of 16 rows j and 16 columns i on and below the diagonal
 #pragma unroll 1
             for (int t = wave; t < 3; t += NW) {
@@ -173,66 +164,78 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
                         for (int I = 0; I < 2; ++I) out[I] = mma(S[y][e], b[I][e], out[I]);
                 }
 #pragma unroll
-                for (int I = 0; I < 2; ++I) out[I] *= scaled[16 * I + l16 + 1];
+                for (int I = 0; I < 2; ++I) out[I] *= scaled[16 * I + l16 + 1] * gain;
             }
             __syncthreads();       // the scores are there
             if (c + 1 < chunks) load(c + 1);        // not before: the operands above need the registers
         }
+        gain *= power[n];
+        const bool small = gain < LA_LEAST_GAIN;
         if (mine) {
-            const float w = power[n];
+            if (small) {
 #pragma unroll
-            for (int y = 0; y < 2 * KT; ++y) S[y] *= w;
+                for (int y = 0; y < 2 * KT; ++y) S[y] *= gain;
+            }
+            f32x4 vv[2];
 #pragma unroll
             for (int s = 0; s < 2; ++s) {
-                f32x4 vv;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) vv[e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
-                if (!STATES) {
-#pragma unroll
-                    for (int I = s; I < 2; ++I) {
-                        const f32x4 p = read4(sp + I * 16 * P_ROW + (p_at ^ (s << 6)));
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) out[I] = mma(strange && !finite(vv[e]) ? 0.f : vv[e], p[e], out[I]);
-                    }
-                }
-                vv *= *reinterpret_cast<const f32x4*>(weight + 16 * s + 4 * g);
+                for (int e = 0; e < 4; ++e) vv[s][e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
+                const f32x4 wv = vv[s] * *reinterpret_cast<const f32x4*>(weight + 16 * s + 4 * g);
 #pragma unroll
                 for (int y = 0; y < 2 * KT; y += 2)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
                         for (int z = 0; z < 2; ++z)
-                            S[y + z] = mma(*reinterpret_cast<const float*>(sk + 16 * s * KR + la_block(k_at[e], y + z)), vv[e], S[y + z]);
+                            S[y + z] = mma(*reinterpret_cast<const float*>(sk + 16 * s * KR + la_block(k_at[e], y + z)), wv[e], S[y + z]);
             }
-        }
-        if (!STATES && mine) {
-            if (strange) {
-                // A value that is not finite, times the zero above the diagonal, would reach steps before its own: such
-                // values were left out of the product and are added here to the steps that they belong to.
+            if (!STATES) {
+                // A value that is not finite, times the zero above the diagonal, would reach steps before its own.  It makes
+                // every row of its column of the state not finite: where one is, such values are left out of the product and
+                // added to the steps that they belong to.
+                const bool strange = __builtin_amdgcn_ballot_w64(!finite(S[0][0])) != 0;
+                if (strange) {
 #pragma unroll 1
-                for (int j = 0; j < C; ++j) {
-                    const f32x4 x = read4(sv + la_piece<VR>(j, 4 * wave + g));
-                    const int place = step_place(j);
+                    for (int j = 0; j < C; ++j) {
+                        const f32x4 x = read4(sv + la_piece<VR>(j, 4 * wave + g));
+                        const int place = step_place(j);
 #pragma unroll
-                    for (int I = 0; I < 2; ++I) {
-                        const int i = 16 * I + l16;
-                        const float p = *reinterpret_cast<const float*>(sp + la_piece<P_ROW>(i, place >> 2) + 4 * (place & 3));
+                        for (int I = 0; I < 2; ++I) {
+                            const int i = 16 * I + l16;
+                            const float p = *reinterpret_cast<const float*>(sp + la_piece<P_ROW>(i, place >> 2) + 4 * (place & 3));
 #pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            if (j <= i && !finite(x[e])) out[I][e] += p * x[e];
+                            for (int e = 0; e < 4; ++e)
+                                if (j <= i && !finite(x[e])) out[I][e] += p * x[e];
+                        }
                     }
+#pragma unroll
+                    for (int s = 0; s < 2; ++s)
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) vv[s][e] = finite(vv[s][e]) ? vv[s][e] : 0.f;
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s)
+#pragma unroll
+                    for (int I = s; I < 2; ++I) {
+                        const f32x4 p = read4(sp + I * 16 * P_ROW + (p_at ^ (s << 6)));
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) out[I] = mma(vv[s][e], p[e], out[I]);
+                    }
+                const __amdgpu_buffer_rsrc_t rows = la_rows(o + (int64_t)c * C * a.os.t, (uint32_t)a.os.t * 4, cols, n);
+                const uint32_t at_o = 16 * wave + 4 * g < cols ? (uint32_t)l16 * (uint32_t)a.os.t * 4 + 64 * wave + 16 * g : 0x80000000u;
+#pragma unroll
+                for (int I = 0; I < 2; ++I) {
+                    la_u32x4 w;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(out[I][e]);
+                    __builtin_amdgcn_raw_buffer_store_b128(w, rows, at_o + 16 * I * (uint32_t)a.os.t * 4, 0, 0);
                 }
             }
-            float* my_o = o + ((int64_t)c * C + l16) * a.os.t + 16 * wave + 4 * g;
-#pragma unroll
-            for (int I = 0; I < 2; ++I)
-                if (16 * I + l16 < n && 16 * wave + 4 * g < cols) *reinterpret_cast<f32x4*>(my_o + 16 * I * a.os.t) = out[I];
         }
+        if (small) gain = 1.f;
         __syncthreads();           // the tiles are used up
-        if (c + 1 < chunks) {
-            if (!STATES && tid == 0) odd[c & 1] = 0;
-            store(c + 1);
-        }
+        if (c + 1 < chunks) store(c + 1, gain);
         __syncthreads();
     }
 
@@ -245,7 +248,7 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int row = 16 * y + 4 * g + e;
-                if (my_col < cols && row < a.Dk) to[state_at + row * dv + my_col] = S[y][e];
+                if (my_col < cols && row < a.Dk) to[state_at + row * dv + my_col] = gain * S[y][e];
             }
     };
     if (STATES) {
