@@ -23,7 +23,9 @@ struct LaArgs {
     float* sT;                 // likewise; may be s0
     const float* powers;       // [H, LA_CHUNK + 1]: decay[h]^n
     const double* log2_decay;  // [H]
-    float* seams;              // [pieces, B, H, Dk, Dv] when pieces > 1: the state that each piece starts from
+    float* seams;              // when pieces > 1: the state that each piece starts from, as the chunk kernels hold it
+                               // [pieces, B, H, vblocks][wave][block of 16 rows][lane][4]: rows 4 (lane / 16) + 0..3 of a block,
+                               // column lane % 16 of the wave's sixteen
     float scale;
     int T, B, H, rep;          // rep: heads that share a head of k and v
     int Dk, Dv;
@@ -50,23 +52,41 @@ inline int la_waves(int Dk, int Dv) {
     return Dk > 128 ? 8 : Dk > 64 && w < 4 ? 4 : w;
 }
 
+// Numbers of one (piece, sequence, head, block of columns) in the seams.
+inline __host__ __device__ int64_t la_seam(int key_tiles, int waves) { return (int64_t)waves * 2 * key_tiles * 256; }
+
 // Where a workgroup of a chunk kernel works.  Workgroups go to the eight XCDs in turn: those that read the same keys
 // (heads that share them, blocks of columns) follow one another on one XCD, whose L2 then serves all but the first.
 struct LaPlace {
     int b, h, hk, v0, t0, t1, len, piece;
 };
 
+// Sequences of a padded batch come longest first, as far as a wave can sort them: the workgroups that start when others have
+// ended are then the short ones.  (57 sequences of 75 to 301 steps, 5 heads: 41 us, 50 in their order.)
+__device__ inline int la_sequence_of_rank(const LaArgs& a, int rank) {
+    if (!a.lengths || a.B > 64) return rank;
+    const int lane = threadIdx.x & 63;
+    const int mine = lane < a.B ? min(max(a.lengths[lane], 0), a.T) : -1;
+    int before = 0;
+    for (int j = 0; j < a.B; ++j) {
+        const int other = __builtin_amdgcn_readlane(mine, j);
+        before += other > mine || (other == mine && j < lane);
+    }
+    return __ffsll((long long)__builtin_amdgcn_ballot_w64(lane < a.B && before == rank)) - 1;
+}
+
 __device__ inline bool la_place(const LaArgs& a, int pieces, int cols, LaPlace* p) {
-    const int64_t units = (int64_t)a.B * (a.H / a.rep) * pieces;
-    const int shared = a.rep * a.vblocks;
-    const int64_t idx = blockIdx.x / 8, unit = idx / shared * 8 + blockIdx.x % 8;
+    // fewer than 2^31 workgroups: 32-bit divisions
+    const uint32_t kv = a.H / a.rep, units = (uint32_t)a.B * kv * pieces, shared = a.rep * a.vblocks;
+    const uint32_t idx = blockIdx.x / 8, turn = idx / shared, unit = turn * 8 + blockIdx.x % 8;
     if (unit >= units) return false;
-    const int r = (int)(idx % shared);
-    p->piece = (int)(unit % pieces);
-    p->hk = (int)(unit / pieces % (a.H / a.rep));
-    p->b = (int)(unit / pieces / (a.H / a.rep));
-    p->h = p->hk * a.rep + r / a.vblocks;
-    p->v0 = r % a.vblocks * cols;
+    const uint32_t r = idx - turn * shared, seq = unit / pieces, head = r / a.vblocks;
+    p->piece = (int)(unit - seq * pieces);
+    p->b = (int)(seq / kv);
+    p->hk = (int)(seq - p->b * kv);
+    p->b = la_sequence_of_rank(a, p->b);
+    p->h = (int)(p->hk * a.rep + head);
+    p->v0 = (int)(r - head * a.vblocks) * cols;
     p->t0 = p->piece * a.piece_steps;
     p->t1 = min(a.T, p->t0 + a.piece_steps);
     int len = a.lengths ? a.lengths[p->b] : a.T;

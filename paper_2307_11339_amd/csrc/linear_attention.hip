@@ -18,6 +18,8 @@
 namespace rnn {
 namespace {
 
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+
 constexpr int STEP_BLOCK = 16;     // steps whose q, k and v are staged in LDS together
 constexpr int STEP_THREADS = 256;
 
@@ -167,36 +169,55 @@ hipError_t la_launch_steps(int dtype, const LaArgs& a, bool wide, hipStream_t st
 
 namespace {
 
-// The pieces of a sequence know what they add to the state; this turns it into the state that each starts from.
-// One thread for four elements of a state; bound by reading and writing the seams once.
-__global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a) {
-    const int64_t per_state = (int64_t)a.Dk * a.Dv, states = (int64_t)a.B * a.H * per_state;
+// The pieces of sequences know what they add to the state; this turns it into the state that each starts from.
+// One thread for four numbers of a state, as the seams hold them; bound by reading and writing the seams once.
+__global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a, int key_tiles, int waves, bool bf16) {
+    const int64_t per = la_seam(key_tiles, waves), all = (int64_t)a.B * a.H * a.vblocks * per;
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-    if (i >= states) return;
-    const int64_t unit = i / per_state;                // Dv is a multiple of 4: the four are of one state
-    const int b = (int)(unit / a.H), h = (int)(unit % a.H);
+    if (i >= all) return;
+    const uint32_t block = (uint32_t)(i / per), in = (uint32_t)(i - block * per);
+    const uint32_t unit = block / a.vblocks, b = unit / a.H, h = unit - b * a.H;
     const int len = min(a.lengths ? a.lengths[b] : a.T, a.T);
     const float decay = (float)exp2((double)a.piece_steps * a.log2_decay[h]);
-    float4 run = make_float4(0.f, 0.f, 0.f, 0.f);
+    f32x4 run = {0.f, 0.f, 0.f, 0.f};
     if (a.s0) {
-        run = *reinterpret_cast<const float4*>(a.s0 + i);
-        *reinterpret_cast<float4*>(a.seams + i) = run;   // the first piece reads it here: sT may be s0
+        const int lane = in >> 2 & 63, y = (in >> 8) % (2 * key_tiles), wave = (in >> 8) / (2 * key_tiles);
+        const int col = (int)(block - unit * a.vblocks) * waves * 16 + wave * 16 + (lane & 15);
+        const int row = bf16 ? 32 * (y >> 1) + 8 * (lane >> 4) + 4 * (y & 1) : 16 * y + 4 * (lane >> 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col < a.Dv && row + e < a.Dk) run[e] = a.s0[((int64_t)unit * a.Dk + row + e) * a.Dv + col];
+        *reinterpret_cast<f32x4*>(a.seams + i) = run;    // the first piece reads it here: sT may be s0
     }
-    for (int p = 1; p < a.pieces && len > p * a.piece_steps; ++p) {
-        float4* at = reinterpret_cast<float4*>(a.seams + p * states + i);
-        const float4 add = *at;
-        run.x = fmaf(decay, run.x, add.x);
-        run.y = fmaf(decay, run.y, add.y);
-        run.z = fmaf(decay, run.z, add.z);
-        run.w = fmaf(decay, run.w, add.w);
-        *at = run;
+    int live = 1;                                      // pieces that have steps to start
+    while (live < a.pieces && len > live * a.piece_steps) ++live;
+    constexpr int AT_ONCE = 8;                         // loads under way together: the sum is short, the way to memory long
+    for (int p0 = 1; p0 < live; p0 += AT_ONCE) {
+        f32x4 add[AT_ONCE];
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) add[j] = *reinterpret_cast<const f32x4*>(a.seams + min(p0 + j, live - 1) * all + i);
+#pragma unroll
+        for (int j = 0; j < AT_ONCE; ++j) {
+            if (p0 + j >= live) break;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) run[e] = fmaf(decay, run[e], add[j][e]);
+            *reinterpret_cast<f32x4*>(a.seams + (p0 + j) * all + i) = run;
+        }
     }
 }
 
-// Workgroups that the pieces of sequences are to make up together: two for each of the 256 compute units.
-constexpr int LA_WORKGROUPS = 512;
-constexpr int LA_FEWEST_STEPS = 32;                // below that, one step after the other
-constexpr int LA_PIECE_STEPS = 256;                // of a piece at least
+// The shortest call that goes in chunks.  A chunk costs the same whether it is full or not: 24 sequences of 8 heads of 128
+// take 12 us in a chunk of up to 64 steps, one step after the other 9.5 (4 steps), 12.7 (8) and 16 (12); 4 sequences of 4 heads
+// of 256 take 14.6 us in a chunk, 12.8 (16 steps) and 17.2 (24) one after the other.
+inline int fewest_steps(int Dk) { return Dk > 128 ? 20 : 10; }
+
+// Pieces of long sequences.  Computing the states at the seams costs about 0.4 of the forward itself, so sequences are
+// cut only until every compute unit has eight waves; twice as many pieces, half as long, pay only where a piece still has many
+// steps.  16 heads of 128: 2048 steps of 16 sequences 160 us whole, 197 in two pieces; 65536 steps of one
+// 371 us in 32 pieces, 408 in 16; 4096 steps 51 us in 16 pieces, 60 in 32.
+constexpr int LA_WAVES = 2048, LA_LONG_WAVES = 4096;       // eight a compute unit; sixteen
+constexpr int LA_LONG_STEPS = 1024;
+constexpr int LA_PIECE_STEPS = 128;                // of a piece at least
 
 struct LaPlan {
     int chunk = 0, vblocks = 1, pieces = 1, piece_steps = 0;
@@ -213,14 +234,16 @@ LaPlan steps_plan(int H, int Dv, int T, int B) {
 
 LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
     (void)dtype;
-    if (T < LA_FEWEST_STEPS) return steps_plan(H, Dv, T, B);
+    if (T < fewest_steps(Dk)) return steps_plan(H, Dv, T, B);
     LaPlan p;
     p.piece_steps = T;
     p.chunk = LA_CHUNK;
     const int cols = 16 * la_waves(Dk, Dv);
     p.vblocks = (Dv + cols - 1) / cols;
     const int64_t units = (int64_t)B * H * p.vblocks;
-    const int64_t want = LA_WORKGROUPS / units, most = T / LA_PIECE_STEPS;
+    const int64_t waves = units * la_waves(Dk, Dv), most = T / LA_PIECE_STEPS;
+    const bool many = waves < LA_WAVES && T * waves / LA_LONG_WAVES >= LA_LONG_STEPS;
+    const int64_t want = (many ? LA_LONG_WAVES : LA_WAVES) / waves;
     const int pieces = (int)(want < most ? want : most);
     if (pieces >= 2) {
         const int chunks = (T + LA_CHUNK - 1) / LA_CHUNK;
@@ -231,11 +254,8 @@ LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
     return p;
 }
 
-// Bytes of the seams of any shape: pieces are cut only while B * H * vblocks * pieces stays within LA_WORKGROUPS.
-size_t seam_bytes(int Dk, int Dv) {
-    const int cols = 16 * la_waves(Dk, Dv);
-    return (size_t)(LA_WORKGROUPS / ((Dv + cols - 1) / cols)) * Dk * Dv * sizeof(float);
-}
+// Bytes of the seams of any shape: pieces are cut only while all waves together stay within LA_LONG_WAVES.
+size_t seam_bytes(int Dk) { return (size_t)LA_LONG_WAVES * la_seam(la_key_tiles(Dk), 1) * sizeof(float); }
 
 int check_shape(int H, int Hkv, int Dk, int Dv, int dtype) {
     if (H < 1 || Hkv < 1 || Dk < 1 || Dv < 1 || H % Hkv != 0 || (dtype != RNN_F32 && dtype != RNN_BF16)) return RNN_EINVAL;
@@ -383,7 +403,7 @@ int rnn_linear_attention_reserve(rnn_linear_attention* l, int T, int B) {
         return RNN_EDEVICE;
     }
     if (device != l->device) return RNN_EINVAL;
-    const size_t bytes = seam_bytes(l->Dk, l->Dv);
+    const size_t bytes = seam_bytes(l->Dk);
     if (hipMalloc((void**)&l->seams, bytes) != hipSuccess) {
         (void)hipGetLastError();
         l->seams = nullptr;
@@ -444,8 +464,8 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
         if (p.pieces > 1) {
             e = chunks(a, kt, nw, true, st);
             if (e == hipSuccess) {
-                const int64_t quads = (int64_t)B * l->H * l->Dk * l->Dv / 4;       // few: pieces are cut where heads are
-                la_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a);
+                const int64_t quads = (int64_t)B * l->H * p.vblocks * la_seam(kt, nw) / 4;     // few: pieces are cut where heads are
+                la_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a, kt, nw, l->dtype == RNN_BF16);
                 e = hipGetLastError();
             }
         }

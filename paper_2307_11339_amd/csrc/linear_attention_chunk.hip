@@ -17,6 +17,8 @@
 // What bounds it: one chunk of 128 x 128 takes a workgroup 100 matrix instructions a wave (3200 cycles a SIMD with two
 // workgroups on a compute unit) and about as long in vector instructions (splitting into bf16 numbers) beside 64 KB of
 // memory traffic.
+#include <type_traits>
+
 #include "common.h"
 #include "linear_attention.h"
 
@@ -138,14 +140,19 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
     // state: element e of result 2 x + p = row 32 x + 8 g + 4 p + e, column l % 16 of the wave's
     const int my_col = 16 * wave + l16;
     const int64_t state_at = ((int64_t)at.b * a.H + at.h) * a.Dk * a.Dv + at.v0;
-    const int64_t states = (int64_t)a.B * a.H * a.Dk * a.Dv;
-    const float* from = nullptr;
-    if (!STATES && live > 0) from = at.piece > 0 || (a.pieces > 1 && a.s0) ? a.seams + at.piece * states : a.s0;
-    if (!STATES && live == 0 && at.piece == 0) from = a.s0;
+    // the state at the start of piece x
+    const auto seam = [&](int x) {
+        return reinterpret_cast<f32x4*>(a.seams + ((((int64_t)x * a.B + at.b) * a.H + at.h) * a.vblocks + at.v0 / DV) * la_seam(KT, NW)) +
+               (wave * 2 * KT) * 64 + lane;
+    };
     f32x4 S[2 * KT];
-    if (from) {
+    if (!STATES && live > 0 && (at.piece > 0 || (a.pieces > 1 && a.s0))) {
+        const f32x4* from = seam(at.piece);
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y) S[y] = from[y * 64];
+    } else if (!STATES && a.s0 && at.piece == 0) {
         // all loads at once, of a place that is there where the state has none
-        const float* col = from + state_at + (my_col < cols ? my_col : 0);
+        const float* col = a.s0 + state_at + (my_col < cols ? my_col : 0);
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y)
 #pragma unroll
@@ -177,30 +184,44 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
         const char* v_a = sv + la_piece<VR>(tr, 2 * wave + (tc >> 1)) + 8 * (tc & 1);
         const char* v_b = sv + la_piece<VR>(tr + 4, 2 * wave + (tc >> 1)) + 8 * (tc & 1);
         if (!STATES) {
-            // scores: blocks of 16 rows j and 16 columns i on and below the diagonal
-#pragma unroll 1
-            for (int t = wave; t < 10; t += NW) {
-                const int I = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, J = t - I * (I + 1) / 2;
-                f32x4 s = {0.f, 0.f, 0.f, 0.f};
+            // scores: blocks of 16 rows j and 16 columns i on and below the diagonal, ten in all; two at a time where a wave
+            // has two, so that one's reads and products fill the other's waits
+            auto scores = [&](int t0, auto blocks) {
+                constexpr int BLOCKS = decltype(blocks)::value;
+                f32x4 s[BLOCKS];
+                int I[BLOCKS], J[BLOCKS];
 #pragma unroll
-                for (int x = 0; x < KT; ++x) {
-                    const bf16x8 kk = read8(sk + J * 16 * KR + la_block(row_at, x));
-                    const bf16x8 qq = read8(sq + I * 16 * KR + la_block(row_at, x));
-                    s = mma(kk, qq, s);
+                for (int z = 0; z < BLOCKS; ++z) {
+                    const int t = t0 + z * NW;
+                    I[z] = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3;
+                    J[z] = t - I[z] * (I[z] + 1) / 2;
+                    s[z] = f32x4{0.f, 0.f, 0.f, 0.f};
                 }
-                const int i = 16 * I + l16, j = 16 * J + 4 * g;
-                float p[4];
 #pragma unroll
-                for (int e = 0; e < 4; ++e) p[e] = i >= j + e ? s[e] * scaled[max(i - j - e, 0)] : 0.f;
-                uint2 hi, lo;
-                hi.x = round2(p[0], p[1]);
-                hi.y = round2(p[2], p[3]);
-                lo.x = round2(p[0], p[1]);
-                lo.y = round2(p[2], p[3]);
-                char* to = sp + la_piece<P_ROW>(i, 2 * J + (g >> 1)) + 8 * (g & 1);
-                *reinterpret_cast<uint2*>(to) = hi;
-                *reinterpret_cast<uint2*>(to + C * P_ROW) = lo;
-            }
+                for (int x = 0; x < KT; ++x)
+#pragma unroll
+                    for (int z = 0; z < BLOCKS; ++z)
+                        s[z] = mma(read8(sk + J[z] * 16 * KR + la_block(row_at, x)), read8(sq + I[z] * 16 * KR + la_block(row_at, x)), s[z]);
+#pragma unroll
+                for (int z = 0; z < BLOCKS; ++z) {
+                    const int i = 16 * I[z] + l16, j = 16 * J[z] + 4 * g;
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = i >= j + e ? s[z][e] * scaled[max(i - j - e, 0)] : 0.f;
+                    uint2 hi, lo;
+                    hi.x = round2(p[0], p[1]);
+                    hi.y = round2(p[2], p[3]);
+                    lo.x = round2(p[0], p[1]);
+                    lo.y = round2(p[2], p[3]);
+                    char* to = sp + la_piece<P_ROW>(i, 2 * J[z] + (g >> 1)) + 8 * (g & 1);
+                    *reinterpret_cast<uint2*>(to) = hi;
+                    *reinterpret_cast<uint2*>(to + C * P_ROW) = lo;
+                }
+            };
+#pragma unroll 1
+            for (int t = wave; t < 10; t += 2 * NW)
+                if (t + NW < 10) scores(t, std::integral_constant<int, 2>());
+                else scores(t, std::integral_constant<int, 1>());
             // what the state before the chunk gives
             if (mine) {
 #pragma unroll
@@ -306,27 +327,28 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
         __syncthreads();
     }
 
-    // the rows' offsets again, not those of the loads above kept in registers all along
-    int dv = a.Dv;
-    asm volatile("" : "+s"(dv));
-    auto write_state = [&](float* to) {
-#pragma unroll
-        for (int y = 0; y < 2 * KT; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = 32 * (y >> 1) + 8 * g + 4 * (y & 1) + e;
-                if (my_col < cols && row < a.Dk) to[state_at + row * dv + my_col] = gain * S[y][e];
-            }
-    };
     if (STATES) {
-        write_state(a.seams + (at.piece + 1) * states);
+        f32x4* to = seam(at.piece + 1);
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y) to[y * 64] = gain * S[y];
         return;
     }
     const int per_row = cols / 8, dead = at.t1 - at.t0 - live;
     for (int64_t i = tid; i < (int64_t)dead * per_row; i += THREADS)
         *reinterpret_cast<uint4*>(o + (live + i / per_row) * a.os.t + i % per_row * 8) = make_uint4(0, 0, 0, 0);
     const bool ends_here = (live > 0 && at.len <= at.t1) || (at.len == 0 && at.piece == 0);
-    if (a.sT && ends_here) write_state(a.sT);
+    if (a.sT && ends_here) {
+        // the rows' offsets again, not those of the loads above kept in registers all along
+        int dv = a.Dv;
+        asm volatile("" : "+s"(dv));
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = 32 * (y >> 1) + 8 * g + 4 * (y & 1) + e;
+                if (my_col < cols && row < a.Dk) a.sT[state_at + row * dv + my_col] = gain * S[y][e];
+            }
+    }
 }
 
 template <bool STATES>

@@ -17,18 +17,17 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-constexpr int C = 32;
-constexpr int P_ROW = 4 * C;          // bytes of a row of scores
-
 __device__ inline f32x4 mma(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 __device__ inline f32x4 read4(const char* p) { return *reinterpret_cast<const f32x4*>(p); }
 __device__ inline bool finite(float x) { return fabsf(x) < __builtin_inff(); }
 // where step j of a chunk stands among scores and weights
-__device__ inline int step_place(int j) { return (j & 16) + 4 * (j & 3) + (j >> 2 & 3); }
+__device__ inline int step_place(int j) { return (j & ~15) + 4 * (j & 3) + (j >> 2 & 3); }
 
 template <int KT, int NW, bool STATES>
 __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(const LaArgs a) {
     constexpr int DK = 32 * KT, DV = 16 * NW, THREADS = 64 * NW;
+    constexpr int C = 32, BLOCKS = C / 16, P_ROW = 4 * C;      // steps of a chunk; bytes of a row of scores
+    static_assert(C <= LA_CHUNK && LA_CHUNK % C == 0, "pieces are whole chunks; powers go as far as LA_CHUNK");
     typedef LaTile<float, C, DK, THREADS> KeyTile;
     typedef LaTile<float, C, DV, THREADS> ValueTile;
     constexpr int KR = KeyTile::ROW, VR = ValueTile::ROW;
@@ -83,22 +82,22 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
         power[i] = p;
         scaled[i] = p * a.scale;
     }
-    if (!STATES) {
-        // the block of scores behind the diagonal that takes part in products: rows 0..15, steps 16..31
-        if (tid < 64) *reinterpret_cast<la_u32x4*>(sp + la_piece<P_ROW>(tid >> 2, 4 + (tid & 3))) = la_u32x4{0, 0, 0, 0};
-    }
-
     // state: element e of result y = row 16 y + 4 g + e, column l % 16 of the wave's
     const int my_col = 16 * wave + l16;
     const int64_t state_at = ((int64_t)at.b * a.H + at.h) * a.Dk * a.Dv + at.v0;
-    const int64_t states = (int64_t)a.B * a.H * a.Dk * a.Dv;
-    const float* from = nullptr;
-    if (!STATES && live > 0) from = at.piece > 0 || (a.pieces > 1 && a.s0) ? a.seams + at.piece * states : a.s0;
-    if (!STATES && live == 0 && at.piece == 0) from = a.s0;
+    // the state at the start of piece x
+    const auto seam = [&](int x) {
+        return reinterpret_cast<f32x4*>(a.seams + ((((int64_t)x * a.B + at.b) * a.H + at.h) * a.vblocks + at.v0 / DV) * la_seam(KT, NW)) +
+               (wave * 2 * KT) * 64 + lane;
+    };
     f32x4 S[2 * KT];
-    if (from) {
+    if (!STATES && live > 0 && (at.piece > 0 || (a.pieces > 1 && a.s0))) {
+        const f32x4* from = seam(at.piece);
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y) S[y] = from[y * 64];
+    } else if (!STATES && a.s0 && at.piece == 0) {
         // all loads at once, of a place that is there where the state has none
-        const float* col = from + state_at + (my_col < cols ? my_col : 0);
+        const float* col = a.s0 + state_at + (my_col < cols ? my_col : 0);
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y)
 #pragma unroll
@@ -120,7 +119,7 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
     for (int c = 0; c < chunks; ++c) {
         const int n = min(C, live - c * C);
         if (STATES && c + 1 < chunks) load(c + 1);
-        f32x4 out[2];
+        f32x4 out[BLOCKS];
         // the lane's places in the tiles; found anew for each chunk: they are cheap, and registers are short
         const int l16 = la_fresh(lane & 15), g = la_fresh(lane >> 4);
         const int row_at = la_piece<KR>(l16, g), p_at = la_piece<P_ROW>(l16, g);
@@ -134,8 +133,8 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
         if (!STATES) {
             // scores: blocks of 16 rows j and 16 columns i on and below the diagonal
 #pragma unroll 1
-            for (int t = wave; t < 3; t += NW) {
-                const int I = t < 1 ? 0 : 1, J = t == 1 ? 1 : 0;
+            for (int t = wave; t < BLOCKS * (BLOCKS + 1) / 2; t += NW) {
+                const int I = t < 1 ? 0 : t < 3 ? 1 : t < 6 ? 2 : 3, J = t - I * (I + 1) / 2;
                 f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int y = 0; y < 2 * KT; ++y) {
@@ -152,19 +151,19 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
             // what the state before the chunk gives
             if (mine) {
 #pragma unroll
-                for (int I = 0; I < 2; ++I) out[I] = f32x4{0.f, 0.f, 0.f, 0.f};
+                for (int I = 0; I < BLOCKS; ++I) out[I] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int y = 0; y < 2 * KT; ++y) {
-                    f32x4 b[2];
+                    f32x4 b[BLOCKS];
 #pragma unroll
-                    for (int I = 0; I < 2; ++I) b[I] = read4(sq + I * 16 * KR + la_block(row_at, y));
+                    for (int I = 0; I < BLOCKS; ++I) b[I] = read4(sq + I * 16 * KR + la_block(row_at, y));
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
-                        for (int I = 0; I < 2; ++I) out[I] = mma(S[y][e], b[I][e], out[I]);
+                        for (int I = 0; I < BLOCKS; ++I) out[I] = mma(S[y][e], b[I][e], out[I]);
                 }
 #pragma unroll
-                for (int I = 0; I < 2; ++I) out[I] *= scaled[16 * I + l16 + 1] * gain;
+                for (int I = 0; I < BLOCKS; ++I) out[I] *= scaled[16 * I + l16 + 1] * gain;
             }
             __syncthreads();       // the scores are there
             if (c + 1 < chunks) load(c + 1);        // not before: the operands above need the registers
@@ -176,9 +175,9 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
 #pragma unroll
                 for (int y = 0; y < 2 * KT; ++y) S[y] *= gain;
             }
-            f32x4 vv[2];
+            f32x4 vv[BLOCKS];
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
+            for (int s = 0; s < BLOCKS; ++s) {
 #pragma unroll
                 for (int e = 0; e < 4; ++e) vv[s][e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
                 const f32x4 wv = vv[s] * *reinterpret_cast<const f32x4*>(weight + 16 * s + 4 * g);
@@ -201,7 +200,7 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
                         const f32x4 x = read4(sv + la_piece<VR>(j, 4 * wave + g));
                         const int place = step_place(j);
 #pragma unroll
-                        for (int I = 0; I < 2; ++I) {
+                        for (int I = 0; I < BLOCKS; ++I) {
                             const int i = 16 * I + l16;
                             const float p = *reinterpret_cast<const float*>(sp + la_piece<P_ROW>(i, place >> 2) + 4 * (place & 3));
 #pragma unroll
@@ -210,22 +209,22 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
                         }
                     }
 #pragma unroll
-                    for (int s = 0; s < 2; ++s)
+                    for (int s = 0; s < BLOCKS; ++s)
 #pragma unroll
                         for (int e = 0; e < 4; ++e) vv[s][e] = finite(vv[s][e]) ? vv[s][e] : 0.f;
                 }
 #pragma unroll
-                for (int s = 0; s < 2; ++s)
+                for (int s = 0; s < BLOCKS; ++s)
 #pragma unroll
-                    for (int I = s; I < 2; ++I) {
-                        const f32x4 p = read4(sp + I * 16 * P_ROW + (p_at ^ (s << 6)));
+                    for (int I = s; I < BLOCKS; ++I) {
+                        const f32x4 p = read4(sp + I * 16 * P_ROW + la_block(p_at, s));
 #pragma unroll
                         for (int e = 0; e < 4; ++e) out[I] = mma(vv[s][e], p[e], out[I]);
                     }
                 const __amdgpu_buffer_rsrc_t rows = la_rows(o + (int64_t)c * C * a.os.t, (uint32_t)a.os.t * 4, cols, n);
                 const uint32_t at_o = 16 * wave + 4 * g < cols ? (uint32_t)l16 * (uint32_t)a.os.t * 4 + 64 * wave + 16 * g : 0x80000000u;
 #pragma unroll
-                for (int I = 0; I < 2; ++I) {
+                for (int I = 0; I < BLOCKS; ++I) {
                     la_u32x4 w;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(out[I][e]);
@@ -239,27 +238,28 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
         __syncthreads();
     }
 
-    // the rows' offsets again, not those of the loads above kept in registers all along
-    int dv = a.Dv;
-    asm volatile("" : "+s"(dv));
-    auto write_state = [&](float* to) {
-#pragma unroll
-        for (int y = 0; y < 2 * KT; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = 16 * y + 4 * g + e;
-                if (my_col < cols && row < a.Dk) to[state_at + row * dv + my_col] = gain * S[y][e];
-            }
-    };
     if (STATES) {
-        write_state(a.seams + (at.piece + 1) * states);
+        f32x4* to = seam(at.piece + 1);
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y) to[y * 64] = gain * S[y];
         return;
     }
     const int per_row = cols / 4, dead = at.t1 - at.t0 - live;
     for (int64_t i = tid; i < (int64_t)dead * per_row; i += THREADS)
         *reinterpret_cast<uint4*>(o + (live + i / per_row) * a.os.t + i % per_row * 4) = make_uint4(0, 0, 0, 0);
     const bool ends_here = (live > 0 && at.len <= at.t1) || (at.len == 0 && at.piece == 0);
-    if (a.sT && ends_here) write_state(a.sT);
+    if (a.sT && ends_here) {
+        // the rows' offsets again, not those of the loads above kept in registers all along
+        int dv = a.Dv;
+        asm volatile("" : "+s"(dv));
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int row = 16 * y + 4 * g + e;
+                if (my_col < cols && row < a.Dk) a.sT[state_at + row * dv + my_col] = gain * S[y][e];
+            }
+    }
 }
 
 template <bool STATES>

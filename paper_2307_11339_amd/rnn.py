@@ -393,12 +393,16 @@ def rnn_model_read_step_ticks(model: int, count: int):
 def _view(t, dims: int):
     """(device address, strides) of a tensor view whose innermost elements lie side by side: its `dims` outer strides, or None
     for what is contiguous or comes as an address."""
-    if t is None or isinstance(t, int):
+    if t is None or type(t) is int:
         return t, None
     if t.is_contiguous():
         return t.data_ptr(), None
-    assert t.dim() == dims + 1 and t.stride(-1) == 1, "a strided tensor needs %d outer dimensions and elements side by side" % dims
-    return t.data_ptr(), (ctypes.c_int64 * dims)(*t.stride()[:dims])
+    strides = t.stride()
+    assert len(strides) == dims + 1 and strides[dims] == 1, "a strided tensor needs %d outer dimensions and elements side by side" % dims
+    return t.data_ptr(), _STRIDES[dims](*strides[:dims])
+
+
+_STRIDES = {2: ctypes.c_int64 * 2, 3: ctypes.c_int64 * 3}
 
 
 def rnn_linear_attention_create(num_heads: int, num_kv_heads: int, key_size: int, value_size: int, dtype: int,
@@ -425,10 +429,14 @@ def rnn_linear_attention_reserve(layer: int, T: int, B: int) -> int:
 def rnn_linear_attention_forward(layer: int, q, k, v, lengths, s0, o, sT, T: int, B: int, stream=None) -> int:
     """Arguments as in include/rnn.h.  q, k, v and o are tensors [T, B, heads, size], whose strides are passed on (slices
     of one projection, transposed batch-first tensors), or addresses of contiguous ones."""
-    s = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
-    (qp, qs), (kp, ks), (vp, vs), (op, os_) = (_view(t, 3) for t in (q, k, v, o))
-    return load_library().rnn_linear_attention_forward(layer, qp, qs, kp, ks, vp, vs, _ptr(lengths), _ptr(s0), op, os_, _ptr(sT),
-                                                       T, B, s)
+    s = stream if stream is None or type(stream) is int else stream.cuda_stream
+    qp, qs = _view(q, 3)
+    kp, ks = _view(k, 3)
+    vp, vs = _view(v, 3)
+    op, os_ = _view(o, 3)
+    return (_lib or load_library()).rnn_linear_attention_forward(
+        layer, qp, qs, kp, ks, vp, vs, None if lengths is None else _ptr(lengths), None if s0 is None else _ptr(s0), op, os_,
+        None if sT is None else _ptr(sT), T, B, s)
 
 
 def rnn_linear_attention_device_bytes(layer: int) -> int:
@@ -466,7 +474,11 @@ def rnn_block_norm_destroy(norm: Optional[int]) -> None:
 def rnn_block_norm_forward(norm: int, x, gate, residual, residual_out, y, lengths, T: int, B: int, stream=None) -> int:
     """Arguments as in include/rnn.h.  x, gate, residual, residual_out and y are tensors [T, B, W], whose strides are passed
     on, or addresses of contiguous ones; gate, residual and one of the outputs may be None."""
-    s = stream.cuda_stream if hasattr(stream, "cuda_stream") else stream
-    views = [_view(t, 2) for t in (x, gate, residual, residual_out, y)]
-    args = [p for pair in views for p in pair]
-    return load_library().rnn_block_norm_forward(norm, *args, _ptr(lengths), T, B, s)
+    s = stream if stream is None or type(stream) is int else stream.cuda_stream
+    xp, xs = _view(x, 2)
+    gp, gs = _view(gate, 2)
+    rp, rs = _view(residual, 2)
+    op, os_ = _view(residual_out, 2)
+    yp, ys = _view(y, 2)
+    return (_lib or load_library()).rnn_block_norm_forward(norm, xp, xs, gp, gs, rp, rs, op, os_, yp, ys,
+                                                           None if lengths is None else _ptr(lengths), T, B, s)
