@@ -73,7 +73,7 @@ __device__ inline void split(const float* x, bf16x8 (&part)[PARTS]) {
 }
 
 template <int KT, int NW, bool STATES>
-__global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(const LaArgs a) {
+__global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW)) void la_chunk_kernel(const LaArgs a) {
     constexpr int DK = 32 * KT, DV = 16 * NW, THREADS = 64 * NW;
     typedef LaTile<bf16_t, C, DK, THREADS> KeyTile;
     typedef LaTile<bf16_t, C, DV, THREADS> ValueTile;
@@ -165,6 +165,9 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_kernel(cons
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y) S[y] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    // the state is waited for here: inside the loop the wait would be for the outputs of the chunk before as well
+#pragma unroll
+    for (int y = 0; y < 2 * KT; ++y) asm volatile("" : "+v"(S[y]));
     __syncthreads();
     if (chunks) store(0, 1.f);
     __syncthreads();

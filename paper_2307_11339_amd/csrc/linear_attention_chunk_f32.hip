@@ -24,7 +24,7 @@ __device__ inline bool finite(float x) { return fabsf(x) < __builtin_inff(); }
 __device__ inline int step_place(int j) { return (j & ~15) + 4 * (j & 3) + (j >> 2 & 3); }
 
 template <int KT, int NW, bool STATES>
-__global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(const LaArgs a) {
+__global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW)) void la_chunk_f32_kernel(const LaArgs a) {
     constexpr int DK = 32 * KT, DV = 16 * NW, THREADS = 64 * NW;
     constexpr int C = 32, BLOCKS = C / 16, P_ROW = 4 * C;      // steps of a chunk; bytes of a row of scores
     static_assert(C <= LA_CHUNK && LA_CHUNK % C == 0, "pieces are whole chunks; powers go as far as LA_CHUNK");
@@ -110,6 +110,9 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y) S[y] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    // the state is waited for here: inside the loop the wait would be for the outputs of the chunk before as well
+#pragma unroll
+    for (int y = 0; y < 2 * KT; ++y) asm volatile("" : "+v"(S[y]));
     __syncthreads();
     if (chunks) store(0, 1.f);
     __syncthreads();
@@ -141,6 +144,7 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
                     const f32x4 kk = read4(sk + J * 16 * KR + la_block(row_at, y)), qq = read4(sq + I * 16 * KR + la_block(row_at, y));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) s = mma(kk[e], qq[e], s);
+                    if (y % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
                 const int i = 16 * I + l16, j = 16 * J + 4 * g;
 #pragma unroll
@@ -175,12 +179,12 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
 #pragma unroll
                 for (int y = 0; y < 2 * KT; ++y) S[y] *= gain;
             }
-            f32x4 vv[BLOCKS];
 #pragma unroll
             for (int s = 0; s < BLOCKS; ++s) {
+                f32x4 wv;
 #pragma unroll
-                for (int e = 0; e < 4; ++e) vv[s][e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
-                const f32x4 wv = vv[s] * *reinterpret_cast<const f32x4*>(weight + 16 * s + 4 * g);
+                for (int e = 0; e < 4; ++e) wv[e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
+                wv *= *reinterpret_cast<const f32x4*>(weight + 16 * s + 4 * g);
 #pragma unroll
                 for (int y = 0; y < 2 * KT; y += 2)
 #pragma unroll
@@ -188,11 +192,17 @@ __global__ __launch_bounds__(64 * NW, KT <= 4 ? 4 : 2) void la_chunk_f32_kernel(
 #pragma unroll
                         for (int z = 0; z < 2; ++z)
                             S[y + z] = mma(*reinterpret_cast<const float*>(sk + 16 * s * KR + la_block(k_at[e], y + z)), wv[e], S[y + z]);
+                __builtin_amdgcn_sched_barrier(0);      // operands of one half at a time: there are no registers for both
             }
             if (!STATES) {
                 // A value that is not finite, times the zero above the diagonal, would reach steps before its own.  It makes
                 // every row of its column of the state not finite: where one is, such values are left out of the product and
                 // added to the steps that they belong to.
+                f32x4 vv[BLOCKS];
+#pragma unroll
+                for (int s = 0; s < BLOCKS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) vv[s][e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
                 const bool strange = __builtin_amdgcn_ballot_w64(!finite(S[0][0])) != 0;
                 if (strange) {
 #pragma unroll 1
