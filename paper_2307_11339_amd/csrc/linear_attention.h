@@ -29,7 +29,7 @@ struct LaArgs {
     float scale;
     int T, B, H, rep;          // rep: heads that share a head of k and v
     int Dk, Dv;
-    int vblocks;               // workgroups that share the Dv columns of one state
+    int vblocks, columns;      // workgroups that share the Dv columns of one state, columns of each but the last
     int pieces, piece_steps;   // pieces of a sequence along time; steps of one (a multiple of LA_CHUNK when pieces > 1)
 };
 
@@ -41,15 +41,21 @@ hipError_t la_launch_steps(int dtype, const LaArgs& a, bool wide, hipStream_t st
 hipError_t la_launch_chunks_bf16(const LaArgs& a, int key_tiles, int waves, bool states, hipStream_t stream);
 hipError_t la_launch_chunks_f32(const LaArgs& a, int key_tiles, int waves, bool states, hipStream_t stream);
 
-// Blocks of 32 rows that a chunk kernel holds of a state, and blocks of 16 columns (waves) of a workgroup.  Rows of
-// wide keys are more than few waves can hold on their way to LDS: these have waves without columns.
+// Blocks of 32 rows that a chunk kernel holds of a state; columns of a workgroup's block of a state; its waves, which take 16
+// columns each.  Rows of wide keys are more than few waves can hold on their way to LDS: these have waves without columns.  So
+// have blocks of five to seven: of workgroups of six waves only one stands on a compute unit at a time, of eight waves two
+// (512 steps of 64 x 32 heads of 96 x 96: 264 us with six waves, 229 with eight, of which two have no columns).
 inline int la_key_tiles(int Dk) {
     const int t = (Dk + 31) / 32;
     return t <= 4 ? t : t <= 6 ? 6 : 8;
 }
+inline int la_columns(int Dv) {
+    const int t = (Dv + 15) / 16, blocks = (t + 7) / 8;
+    return (t + blocks - 1) / blocks * 16;
+}
 inline int la_waves(int Dk, int Dv) {
-    const int t = (Dv + 15) / 16, blocks = (t + 7) / 8, w = ((t + blocks - 1) / blocks + 1) / 2 * 2;
-    return Dk > 128 ? 8 : Dk > 64 && w < 4 ? 4 : w;
+    const int w = la_columns(Dv) / 16;
+    return Dk > 128 || w > 4 ? 8 : Dk > 64 || w > 2 ? 4 : 2;
 }
 
 // Numbers of one (piece, sequence, head, block of columns) in the seams.
@@ -81,7 +87,7 @@ __device__ inline int la_sequence_of_rank(const LaArgs& a, int rank) {
     return __ffsll((long long)__builtin_amdgcn_ballot_w64(lane < a.B && before == rank)) - 1;
 }
 
-__device__ inline bool la_place(const LaArgs& a, int pieces, int cols, LaPlace* p) {
+__device__ inline bool la_place(const LaArgs& a, int pieces, LaPlace* p) {
     // fewer than 2^31 workgroups: 32-bit divisions
     const uint32_t kv = a.H / a.rep, units = (uint32_t)a.B * kv * pieces, shared = a.rep * a.vblocks;
     const uint32_t idx = blockIdx.x / 8, turn = idx / shared, unit = turn * 8 + blockIdx.x % 8;
@@ -92,7 +98,7 @@ __device__ inline bool la_place(const LaArgs& a, int pieces, int cols, LaPlace* 
     p->hk = (int)(seq - p->b * kv);
     p->b = la_sequence_of_rank(a, p->b);
     p->h = (int)(p->hk * a.rep + head);
-    p->v0 = (int)(r - head * a.vblocks) * cols;
+    p->v0 = (int)(r - head * a.vblocks) * a.columns;
     p->t0 = p->piece * a.piece_steps;
     p->t1 = min(a.T, p->t0 + a.piece_steps);
     int len = a.lengths ? a.lengths[p->b] : a.T;

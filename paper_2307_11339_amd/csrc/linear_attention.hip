@@ -182,11 +182,11 @@ __global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a, int key_ti
     f32x4 run = {0.f, 0.f, 0.f, 0.f};
     if (a.s0) {
         const int lane = in >> 2 & 63, y = (in >> 8) % (2 * key_tiles), wave = (in >> 8) / (2 * key_tiles);
-        const int col = (int)(block - unit * a.vblocks) * waves * 16 + wave * 16 + (lane & 15);
+        const int col = (int)(block - unit * a.vblocks) * a.columns + wave * 16 + (lane & 15);
         const int row = bf16 ? 32 * (y >> 1) + 8 * (lane >> 4) + 4 * (y & 1) : 16 * y + 4 * (lane >> 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (col < a.Dv && row + e < a.Dk) run[e] = a.s0[((int64_t)unit * a.Dk + row + e) * a.Dv + col];
+            if (wave * 16 < a.columns && col < a.Dv && row + e < a.Dk) run[e] = a.s0[((int64_t)unit * a.Dk + row + e) * a.Dv + col];
         *reinterpret_cast<f32x4*>(a.seams + i) = run;    // the first piece reads it here: sT may be s0
     }
     int live = 1;                                      // pieces that have steps to start
@@ -220,7 +220,7 @@ constexpr int LA_LONG_STEPS = 1024;
 constexpr int LA_PIECE_STEPS = 128;                // of a piece at least
 
 struct LaPlan {
-    int chunk = 0, vblocks = 1, pieces = 1, piece_steps = 0;
+    int chunk = 0, vblocks = 1, columns = 0, pieces = 1, piece_steps = 0;
     bool wide = false;
 };
 
@@ -228,7 +228,8 @@ LaPlan steps_plan(int H, int Dv, int T, int B) {
     LaPlan p;
     p.piece_steps = T;
     p.wide = (int64_t)B * H * ((Dv + 127) / 128) >= 512;
-    p.vblocks = p.wide ? (Dv + 127) / 128 : (Dv + 31) / 32;
+    p.columns = p.wide ? 128 : 32;
+    p.vblocks = (Dv + p.columns - 1) / p.columns;
     return p;
 }
 
@@ -238,8 +239,8 @@ LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
     LaPlan p;
     p.piece_steps = T;
     p.chunk = LA_CHUNK;
-    const int cols = 16 * la_waves(Dk, Dv);
-    p.vblocks = (Dv + cols - 1) / cols;
+    p.columns = la_columns(Dv);
+    p.vblocks = (Dv + p.columns - 1) / p.columns;
     const int64_t units = (int64_t)B * H * p.vblocks;
     const int64_t waves = units * la_waves(Dk, Dv), most = T / LA_PIECE_STEPS;
     const bool many = waves < LA_WAVES && T * waves / LA_LONG_WAVES >= LA_LONG_STEPS;
@@ -454,7 +455,7 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
     a.powers = l->powers; a.log2_decay = l->log2_decay; a.seams = l->seams;
     a.scale = l->scale;
     a.T = T; a.B = B; a.H = l->H; a.rep = l->H / l->Hkv; a.Dk = l->Dk; a.Dv = l->Dv;
-    a.vblocks = p.vblocks; a.pieces = p.pieces; a.piece_steps = p.piece_steps;
+    a.vblocks = p.vblocks; a.columns = p.columns; a.pieces = p.pieces; a.piece_steps = p.piece_steps;
     hipError_t e = hipSuccess;
     if (!p.chunk) {
         e = la_launch_steps(l->dtype, a, p.wide, st);

@@ -39,13 +39,13 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW)) void la_chunk_f32
 
     LaPlace at;
     const int pieces = STATES ? a.pieces - 1 : a.pieces;
-    if (!la_place(a, pieces, DV, &at)) return;
+    if (!la_place(a, pieces, &at)) return;
     if (STATES && at.len <= at.t1) return;         // nothing live behind this piece: nobody asks for its state
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int l16 = lane & 15, g = lane >> 4;
     const int live = min(max(at.len - at.t0, 0), at.t1 - at.t0);
-    const int cols = min(DV, a.Dv - at.v0);
-    const bool mine = 16 * wave < cols;            // the last waves of the last block of columns may have none
+    const int cols = min(a.columns, a.Dv - at.v0);        // at most DV
+    const bool mine = 16 * wave < cols;            // the last waves may have none
 
     const float* q = (const float*)a.q + at.b * a.qs.b + at.h * a.qs.h + at.t0 * a.qs.t;
     const float* k = (const float*)a.k + at.b * a.ks.b + at.hk * a.ks.h + at.t0 * a.ks.t;
@@ -87,7 +87,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW)) void la_chunk_f32
     const int64_t state_at = ((int64_t)at.b * a.H + at.h) * a.Dk * a.Dv + at.v0;
     // the state at the start of piece x
     const auto seam = [&](int x) {
-        return reinterpret_cast<f32x4*>(a.seams + ((((int64_t)x * a.B + at.b) * a.H + at.h) * a.vblocks + at.v0 / DV) * la_seam(KT, NW)) +
+        return reinterpret_cast<f32x4*>(a.seams + ((((int64_t)x * a.B + at.b) * a.H + at.h) * a.vblocks + at.v0 / a.columns) * la_seam(KT, NW)) +
                (wave * 2 * KT) * 64 + lane;
     };
     f32x4 S[2 * KT];
@@ -277,10 +277,10 @@ bool launch(const LaArgs& a, int kt, int nw, hipStream_t stream) {
     const unsigned grid = (unsigned)la_grid(a, STATES ? a.pieces - 1 : a.pieces);
 #define LA_CHUNK_CASE(K, N) \
     if (kt == K && nw == N) { la_chunk_f32_kernel<K, N, STATES><<<grid, 64 * N, 0, stream>>>(a); return true; }
-    LA_CHUNK_CASE(1, 2) LA_CHUNK_CASE(1, 4) LA_CHUNK_CASE(1, 6) LA_CHUNK_CASE(1, 8)
-    LA_CHUNK_CASE(2, 2) LA_CHUNK_CASE(2, 4) LA_CHUNK_CASE(2, 6) LA_CHUNK_CASE(2, 8)
-    LA_CHUNK_CASE(3, 4) LA_CHUNK_CASE(3, 6) LA_CHUNK_CASE(3, 8)
-    LA_CHUNK_CASE(4, 4) LA_CHUNK_CASE(4, 6) LA_CHUNK_CASE(4, 8)
+    LA_CHUNK_CASE(1, 2) LA_CHUNK_CASE(1, 4) LA_CHUNK_CASE(1, 8)
+    LA_CHUNK_CASE(2, 2) LA_CHUNK_CASE(2, 4) LA_CHUNK_CASE(2, 8)
+    LA_CHUNK_CASE(3, 4) LA_CHUNK_CASE(3, 8)
+    LA_CHUNK_CASE(4, 4) LA_CHUNK_CASE(4, 8)
     LA_CHUNK_CASE(6, 8) LA_CHUNK_CASE(8, 8)
 #undef LA_CHUNK_CASE
     return false;
