@@ -266,9 +266,9 @@ int check_shape(int H, int Hkv, int Dk, int Dv, int dtype) {
 }
 
 int check_call(int H, int T, int B, const LaPlan& p) {
-    if ((int64_t)T * B > ((int64_t)1 << 30) || (int64_t)B * H * p.pieces > ((int64_t)1 << 30)) return RNN_EUNSUPPORTED;
-    if ((int64_t)B * H * p.pieces * p.vblocks > 0x7fffffffLL) return RNN_EUNSUPPORTED;      // workgroups of one launch
-    return RNN_OK;
+    if ((int64_t)T * B > ((int64_t)1 << 30)) return RNN_EUNSUPPORTED;
+    // workgroups of one launch, of 512 threads at most: with what la_grid adds, fewer than 2^32 threads
+    return (int64_t)B * H * p.pieces * p.vblocks > (1 << 22) ? RNN_EUNSUPPORTED : RNN_OK;
 }
 
 // The strides of a [T, B, heads, size] tensor; false if they cannot be read in 16-byte pieces.  The stride of a dimension of

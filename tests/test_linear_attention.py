@@ -4,7 +4,7 @@ Tolerances.  With M = the formula with absolute values of q, k, v and s0 put in 
   - sums and powers of decays in fp32: at most one rounding, 2^-24, for every term that a result passes through; a term
     passes through at most T + Dk + 64 additions and multiplications;
   - bf16 products of a chunk: scores, the state as an operand and the weighted values are each handed over as two bf16
-    numbers, which leaves 2^-16 of each (2^-8 of what 2^-8 left): 3 * 2^-16 for an output, 2^-16 for a state;
+    numbers or more, which leaves at most 2^-16 of each (2^-8 of what 2^-8 left): 3 * 2^-16 for an output, 2^-16 for a state;
   - the output's own rounding: 2^-8 (bf16) or 2^-24 (fp32) of it.
 """
 import ctypes
@@ -432,3 +432,108 @@ def test_states_beyond_two_to_the_31_elements(gpu):
         ref_o, ref_s = _reference(q64, k64, v64, one.decay, one.scale, one.clamped, s64)
         tol_o, tol_s = _tolerances(BF16, q64, k64, v64, one.decay, one.scale, one.clamped, s64, ref_o)
         assert (abs(one.host(o[:, b:b + 1]) - ref_o) <= tol_o).all() and (abs(one.host(s[b:b + 1]) - ref_s) <= tol_s).all()
+
+
+def test_as_many_workgroups_as_a_launch_has():
+    q = rnn.rnn_linear_attention_plan_query
+    assert q(16, 16, 8, 8, BF16, 1, 1 << 18)[0] == rnn.RNN_OK
+    assert q(16, 16, 8, 8, BF16, 1, (1 << 18) + 1)[0] == rnn.RNN_EUNSUPPORTED
+    assert q(16, 16, 8, 256, BF16, 100, 1 << 17)[0] == rnn.RNN_OK                   # two workgroups a state
+    assert q(16, 16, 8, 256, BF16, 100, (1 << 17) + 1)[0] == rnn.RNN_EUNSUPPORTED
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("T", [1, 12])
+def test_as_many_states_as_are_taken(gpu, T):
+    torch = gpu
+    B, H, D = 1 << 18, 16, 8
+    c = Case(T, 1, H, H, D, D, BF16, state=False)
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+    q, k, v = (x.expand(-1, B, -1, -1) for x in (c.q, c.k, c.v))
+    o = torch.full((T, B, H, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    assert rnn.rnn_linear_attention_forward(c.handle, q, k, v, None, None, o, None, T, B, torch.cuda.current_stream()) == rnn.RNN_OK
+    torch.cuda.synchronize()
+    assert torch.equal(o, o[:, :1].expand(-1, B, -1, -1))
+    c.o = o[:, :1].contiguous()
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Hkv,Dk,Dv,lengths", [
+    (3000, 3, 2, 1, 96, 160, [3000, 300, 0]),             # a sequence that ends in an early piece, one that has no steps
+    (2200, 2, 3, 3, 64, 256, [1, 2200]),
+    (4096, 1, 1, 1, 256, 136, [4033]),                    # the last chunk has one step
+    (1500, 5, 1, 1, 40, 40, [1500, 1500, 128, 129, 1500]),
+])
+def test_pieces_of_padded_sequences_with_the_state_in_place(gpu, T, B, H, Hkv, Dk, Dv, lengths, dtype):
+    c = Case(T, B, H, Hkv, Dk, Dv, dtype, lengths, layout="batch")
+    assert rnn.rnn_linear_attention_plan_query(H, Hkv, Dk, Dv, dtype, T, B)[1]["pieces"] > 1
+    s0 = c.s0.clone()
+    c.sT = c.s0
+    assert c.forward() == rnn.RNN_OK
+    c.s0 = s0
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("lengths", [[50] * 64, [0] * 64, [(11 * b) % 51 for b in range(64)], [50 - b % 3 for b in range(65)]],
+                         ids=["alike", "empty", "mixed", "more_than_a_wave"])
+def test_sequences_in_the_order_of_their_lengths(gpu, lengths, dtype):
+    c = Case(50, len(lengths), 1, 1, 32, 32, dtype, lengths)
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("which", ["q", "k", "v"])
+def test_inputs_repeated_along_time_heads_and_sequences(gpu, which, dtype):
+    for expand in ((40, -1, -1, -1), (-1, 3, -1, -1), (-1, -1, 2, -1)):
+        c = Case(40, 3, 2, 2, 64, 48, dtype)
+        x = getattr(c, which)
+        first = [x[:1], x[:, :1], x[:, :, :1]][[n > 0 for n in expand].index(True)]
+        setattr(c, which, first.expand(*expand))
+        assert c.forward() == rnn.RNN_OK
+        c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_steps_far_apart(gpu, dtype):
+    """32 MiB and a little from step to step: the largest distances that chunks take, and the first that they do not."""
+    torch = gpu
+    T, D = 20, 64
+    one = 16 // (2 if dtype == BF16 else 4)               # elements of 16 bytes
+    for far in ((1 << 21) * one - one, (1 << 21) * one, (1 << 21) * one + one):
+        c = Case(T, 1, 1, 1, D, D, dtype)
+        buf = torch.empty((T - 1) * far + D, dtype=c.tdt, device="cuda")
+        k = torch.as_strided(buf, (T, 1, 1, D), (far, 8, 8, 1))
+        k.copy_(c.k)
+        c.k = k
+        out = torch.full(((T - 1) * far + D,), 7.0, dtype=c.tdt, device="cuda")
+        c.o = torch.as_strided(out, (T, 1, 1, D), (far, 8, 8, 1))
+        assert c.forward() == rnn.RNN_OK
+        c.check()
+        c.o.fill_(7.0)
+        assert bool((out == 7.0).all())                   # nothing was written between the rows
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_without_initial_state_or_new_state(gpu, dtype):
+    for T in (1, 70, 1500):
+        c = Case(T, 2, 2, 2, 64, 64, dtype)
+        assert c.forward() == rnn.RNN_OK
+        c.check()
+        o, s0 = c.o.clone(), c.s0
+        c.o.fill_(7.0)
+        sT, c.sT = c.sT, None
+        assert c.forward() == rnn.RNN_OK
+        c.torch.cuda.synchronize()
+        assert c.torch.equal(c.o, o)
+        c.sT, c.s0 = sT, None
+        assert c.forward() == rnn.RNN_OK
+        c.check()
