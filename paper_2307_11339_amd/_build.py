@@ -42,6 +42,9 @@ NO_SPILL = {"wavefront_x.hip": ("wavefront_x_kernel", "ELi2ELb"),     # file: (k
 # The variants of the XCD-resident kernel hold up to 128 registers of weights a wave (250 of 256 in use): a spill there goes
 # through memory in every step (2 bf16 layers of 512 units, both directions: 659 -> 5197 us).
 NO_SPILL.update({"wavefront_xcd%s.hip" % part: ("wavefront_xcd_kernel", "") for part in ("", "_b", "_c", "_d", "_e", "_f", "_g", "_h", "_i", "_j", "_k", "_l")})
+# The chunks of linear attention hold a state in registers and load the chunk to come while they work on one: a register that is
+# spilled on its way makes that load a wait.
+NO_SPILL.update({"linear_attention_chunk.hip": ("la_chunk_kernel", ""), "linear_attention_chunk_f32.hip": ("la_chunk_f32_kernel", "")})
 
 
 def _check_no_spill(src: str, remarks: str) -> None:

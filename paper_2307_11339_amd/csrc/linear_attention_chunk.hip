@@ -73,7 +73,7 @@ __device__ inline void split(const float* x, bf16x8 (&part)[PARTS]) {
 }
 
 template <int KT, int NW, bool STATES>
-__global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW)) void la_chunk_kernel(const LaArgs a) {
+__global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_chunk_kernel(const LaArgs a) {
     constexpr int DK = 32 * KT, DV = 16 * NW, THREADS = 64 * NW;
     typedef LaTile<bf16_t, C, DK, THREADS> KeyTile;
     typedef LaTile<bf16_t, C, DV, THREADS> ValueTile;
