@@ -82,8 +82,9 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
     __shared__ __attribute__((aligned(1024))) char sk[KeyTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sv[ValueTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sp[STATES ? 16 : 2 * C * P_ROW];       // scores [i][j]: rounded, rest
-    __shared__ __attribute__((aligned(16))) float power[C + 4], scaled[C + 4], weight[C];
+    __shared__ __attribute__((aligned(16))) float power[C + 4], before[16 + C + 4], weight[C];
 
+    float* const scaled = before + 16;             // scale decay^i, and zeros for scores behind the diagonal
     LaPlace at;
     const int pieces = STATES ? a.pieces - 1 : a.pieces;
     if (!la_place(a, pieces, &at)) return;
@@ -129,6 +130,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         power[i] = p;
         scaled[i] = p * a.scale;
     }
+    if (tid < 16) before[tid] = 0.f;
     if (!STATES) {
         // the blocks of scores behind the diagonal that take part in products of 32 steps: rows 0, columns 1 and 2, 3 of 16
         for (int i = tid; i < 2 * 2 * 16 * 2; i += THREADS) {
@@ -210,7 +212,12 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                     const int i = 16 * I[z] + l16, j = 16 * J[z] + 4 * g;
                     float p[4];
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) p[e] = i >= j + e ? s[z][e] * scaled[max(i - j - e, 0)] : 0.f;
+                    for (int e = 0; e < 4; ++e) p[e] = scaled[i - j - e];
+                    // all are read: a condition at each read would be a branch and a wait at each
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(p[e]));
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = i >= j + e ? s[z][e] * p[e] : 0.f;
                     uint2 hi, lo;
                     hi.x = round2(p[0], p[1]);
                     hi.y = round2(p[2], p[3]);

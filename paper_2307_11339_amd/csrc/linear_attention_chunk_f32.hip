@@ -35,8 +35,9 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
     __shared__ __attribute__((aligned(1024))) char sk[KeyTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sv[ValueTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sp[STATES ? 16 : C * P_ROW];           // scores [i][j]
-    __shared__ __attribute__((aligned(16))) float power[C + 4], scaled[C + 4], weight[C];
+    __shared__ __attribute__((aligned(16))) float power[C + 4], before[16 + C + 4], weight[C];
 
+    float* const scaled = before + 16;             // scale decay^i, and zeros for scores behind the diagonal
     LaPlace at;
     const int pieces = STATES ? a.pieces - 1 : a.pieces;
     if (!la_place(a, pieces, &at)) return;
@@ -82,6 +83,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         power[i] = p;
         scaled[i] = p * a.scale;
     }
+    if (tid < 16) before[tid] = 0.f;
     // state: element e of result y = row 16 y + 4 g + e, column l % 16 of the wave's
     const int my_col = 16 * wave + l16;
     const int64_t state_at = ((int64_t)at.b * a.H + at.h) * a.Dk * a.Dv + at.v0;
@@ -147,10 +149,15 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                     if (y % 4 == 3) __builtin_amdgcn_sched_barrier(0);
                 }
                 const int i = 16 * I + l16, j = 16 * J + 4 * g;
+                float p[4];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) p[e] = scaled[i - j - e];
+                // all are read: a condition at each read would be a branch and a wait at each
+#pragma unroll
+                for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(p[e]));
 #pragma unroll
                 for (int e = 0; e < 4; ++e)
-                    *reinterpret_cast<float*>(sp + la_piece<P_ROW>(i, 4 * J + e) + 4 * g) =       // place 16 J + 4 e + g
-                        i >= j + e ? s[e] * scaled[max(i - j - e, 0)] : 0.f;
+                    *reinterpret_cast<float*>(sp + la_piece<P_ROW>(i, 4 * J + e) + 4 * g) = i >= j + e ? s[e] * p[e] : 0.f;       // place 16 J + 4 e + g
             }
             // what the state before the chunk gives
             if (mine) {
