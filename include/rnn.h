@@ -413,6 +413,7 @@ int rnn_linear_attention_reserve(rnn_linear_attention* layer, int T, int B);
  * DEVICE pointers, 16-byte aligned.  o must not overlap an input.  The call enqueues work on `stream` and returns.
  * It allocates device memory only the first time that a shape uses the workspace (see rnn_linear_attention_reserve).
  * Non-finite inputs reach the outputs that depend on them by the formula, and no others (an infinity may come out as NaN).
+ * States are held up to 2^10 times as large while the call runs: finite ones beyond 2^117 may overflow.
  * Stream capture: may be recorded into a HIP graph; RNN_EUNSUPPORTED, with nothing recorded, if the workspace would have to be
  * allocated first.  One forward in flight per layer (a replay counts), as the workspace is the layer's.
  * RNN_EINVAL if the layer belongs to another device than the current one.  RNN_EUNSUPPORTED if T * B > 2^30 or
