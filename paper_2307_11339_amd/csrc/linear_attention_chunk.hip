@@ -16,10 +16,11 @@
 //
 // What bounds it: the issue of instructions.  A chunk of 128 x 128 takes each of eight waves 97 matrix instructions (of 16
 // cycles) and about 500 vector instructions (of 4 cycles; most of them split numbers) beside 64 KB of memory traffic, and of
-// the two kinds little overlaps: alone they took 520 and 330 cycles, together on one SIMD 757.  2048 steps of 32 sequences, 16
-// heads: 261 us at 2.07 GHz, the clock under this load, the matrix units 37 % of it busy, the vector units 49 %; the memory
-// traffic alone would take 210.  All extra bf16 numbers dropped: 241.  Where one workgroup a compute unit works by itself
-// (a prompt, a padded batch) a chunk takes 4.2 us, most of it waiting for LDS and at three barriers.
+// the two kinds little overlaps: in a loop of their own 520 and 330 cycles, together on one SIMD 757.  2048 steps of 32
+// sequences, 16 heads: 261 us at 2.07 GHz, the clock under this load, the matrix units 37 % of it busy, the vector units 49 %.
+// A copy of as many bytes takes 210, the loads and stores of this kernel without its products 229, the kernel without the extra
+// bf16 numbers 241; four waves of 32 columns with 32 x 32 tiles took 279 between other calls, this 272.  Where one workgroup
+// works by itself on a compute unit (a prompt, a padded batch), a chunk takes 4.2 us, most of it waiting for LDS and at barriers.
 #include <type_traits>
 
 #include "common.h"
