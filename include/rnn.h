@@ -432,6 +432,7 @@ size_t rnn_linear_attention_device_bytes(const rnn_linear_attention* layer);
  *   plan[1]  workgroups that share the Dv columns of one state
  *   plan[2]  pieces that a sequence is split into along time
  *   plan[3]  steps of a piece
+ * (Tensors repeated along time, or with 32 MiB and more from step to step, go one step after the other whatever it says.)
  * Errors as rnn_linear_attention_create. */
 int rnn_linear_attention_plan_query(int num_heads, int num_kv_heads, int key_size, int value_size, int dtype, int T,
                                     int B, int* plan);

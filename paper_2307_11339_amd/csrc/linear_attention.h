@@ -6,7 +6,8 @@
 
 namespace rnn {
 
-constexpr int LA_CHUNK = 64;   // steps that the chunk kernels take at once
+constexpr int LA_CHUNK = 64;       // steps that the bf16 chunk kernel takes at once, and of which pieces are multiples
+constexpr int LA_CHUNK_F32 = 32;   // the fp32 one
 
 struct LaView {                // a [T, B, heads, size] tensor: strides in elements
     int64_t t, b, h;

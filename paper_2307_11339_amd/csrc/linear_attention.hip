@@ -235,11 +235,10 @@ LaPlan steps_plan(int H, int Dv, int T, int B) {
 }
 
 LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
-    (void)dtype;
     if (T < fewest_steps(Dk)) return steps_plan(H, Dv, T, B);
     LaPlan p;
     p.piece_steps = T;
-    p.chunk = LA_CHUNK;
+    p.chunk = dtype == RNN_BF16 ? LA_CHUNK : LA_CHUNK_F32;
     p.columns = la_columns(Dv);
     p.vblocks = (Dv + p.columns - 1) / p.columns;
     const int64_t units = (int64_t)B * H * p.vblocks;

@@ -26,7 +26,7 @@ __device__ inline int step_place(int j) { return (j & ~15) + 4 * (j & 3) + (j >>
 template <int KT, int NW, bool STATES>
 __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_chunk_f32_kernel(const LaArgs a) {
     constexpr int DK = 32 * KT, DV = 16 * NW, THREADS = 64 * NW;
-    constexpr int C = 32, BLOCKS = C / 16, P_ROW = 4 * C;      // steps of a chunk; bytes of a row of scores
+    constexpr int C = LA_CHUNK_F32, BLOCKS = C / 16, P_ROW = 4 * C;      // steps of a chunk; bytes of a row of scores
     static_assert(C <= LA_CHUNK && LA_CHUNK % C == 0, "pieces are whole chunks; powers go as far as LA_CHUNK");
     typedef LaTile<float, C, DK, THREADS> KeyTile;
     typedef LaTile<float, C, DV, THREADS> ValueTile;

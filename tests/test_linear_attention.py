@@ -67,10 +67,10 @@ def test_plan_query():
                 for B in (1, 7, 64, 1000):
                     rc, p = q(H, H, Dk, Dv, dtype, T, B)
                     assert rc == rnn.RNN_OK
-                    assert p["chunk"] in (0, 64) and p["value_blocks"] >= 1
+                    assert p["chunk"] in (0, 64 if dtype == BF16 else 32) and p["value_blocks"] >= 1
                     # the pieces cover the sequence, none is empty, and inner seams lie between chunks
                     assert (p["pieces"] - 1) * p["piece_steps"] < T <= p["pieces"] * p["piece_steps"]
-                    assert p["pieces"] == 1 or (p["chunk"] == 64 and p["piece_steps"] % 64 == 0)
+                    assert p["pieces"] == 1 or (p["chunk"] and p["piece_steps"] % 64 == 0)
     assert q(8, 8, 128, 128, BF16, 1, 1)[1]["chunk"] == 0          # a single token has no use for a chunk
 
 
