@@ -76,13 +76,11 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         }
     };
     const int chunks = (live + C - 1) / C;
+    // loads come back in order: this one first, then the first tiles and the state, nothing waited for between them
+    static_assert(THREADS > C, "a thread for each power");
+    const float my_power = a.powers[at.h * (LA_CHUNK + 1) + min(tid, C)];
     if (chunks) load(0);
 
-    for (int i = tid; i <= C; i += THREADS) {
-        const float p = a.powers[at.h * (LA_CHUNK + 1) + i];
-        power[i] = p;
-        scaled[i] = p * a.scale;
-    }
     if (tid < 16) before[tid] = 0.f;
     // state: element e of result y = row 16 y + 4 g + e, column l % 16 of the wave's
     const int my_col = 16 * wave + l16;
@@ -115,6 +113,10 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
     // the state is waited for here: inside the loop the wait would be for the outputs of the chunk before as well
 #pragma unroll
     for (int y = 0; y < 2 * KT; ++y) asm volatile("" : "+v"(S[y]));
+    if (tid <= C) {
+        power[tid] = my_power;
+        scaled[tid] = my_power * a.scale;
+    }
     __syncthreads();
     if (chunks) store(0, 1.f);
     __syncthreads();
