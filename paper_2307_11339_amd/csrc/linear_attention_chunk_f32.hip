@@ -96,16 +96,13 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y) S[y] = from[y * 64];
     } else if (!STATES && a.s0 && at.piece == 0) {
-        // all loads at once, of a place that is there where the state has none
-        const float* col = a.s0 + state_at + (my_col < cols ? my_col : 0);
+        const __amdgpu_buffer_rsrc_t rows = la_rows(a.s0 + state_at, 4 * a.Dv, cols, a.Dk);
+        const uint32_t first = my_col < cols ? (uint32_t)(4 * g * a.Dv + my_col) * 4 : 0x80000000u;
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) S[y][e] = col[min(16 * y + 4 * g + e, a.Dk - 1) * a.Dv];
-#pragma unroll
-        for (int y = 0; y < 2 * KT; ++y)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) S[y][e] = my_col < cols && 16 * y + 4 * g + e < a.Dk ? S[y][e] : 0.f;
+            for (int e = 0; e < 4; ++e)
+                S[y][e] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rows, first + (16 * y + e) * 4 * a.Dv, 0, 0));
     } else {
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y) S[y] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -271,13 +268,13 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         // the rows' offsets again, not those of the loads above kept in registers all along
         int dv = a.Dv;
         asm volatile("" : "+s"(dv));
+        const __amdgpu_buffer_rsrc_t rows = la_rows(a.sT + state_at, 4 * dv, cols, a.Dk);
+        const uint32_t first = my_col < cols ? (uint32_t)(4 * g * dv + my_col) * 4 : 0x80000000u;
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int row = 16 * y + 4 * g + e;
-                if (my_col < cols && row < a.Dk) a.sT[state_at + row * dv + my_col] = gain * S[y][e];
-            }
+            for (int e = 0; e < 4; ++e)
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(gain * S[y][e]), rows, first + (16 * y + e) * 4 * dv, 0, 0);
     }
 }
 
