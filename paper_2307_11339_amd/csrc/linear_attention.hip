@@ -207,9 +207,11 @@ __global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a, int key_ti
 }
 
 // The shortest call that goes in chunks.  A chunk costs the same whether it is full or not: 24 sequences of 8 heads of 128
-// take 12 us in a chunk of up to 64 steps, one step after the other 9.5 (4 steps), 12.7 (8) and 16 (12); 4 sequences of 4 heads
-// of 256 take 14.6 us in a chunk, 12.8 (16 steps) and 17.2 (24) one after the other.
-inline int fewest_steps(int Dk) { return Dk > 128 ? 20 : 10; }
+// take 11 us in a chunk of up to 64 steps, one step after the other 9.4 (4 steps), 11 (6), 12.8 (8) and 14.3 (10); 64 sequences of 8
+// heads of 64 8.8, and 8.1 (4), 9.1 (6); in fp32 24 of 8 heads of 128 13.6, and 11.6 (6), 13 (8), 15 (10).  One sequence alone takes 8.2
+// us in a chunk, 6.3 (6) and 8.3 (12) one after the other.  4 sequences of 4 heads of 256 take 11.6 us in a chunk, 11 (12 steps) and
+// 12.8 (16) one after the other.
+inline int fewest_steps(int Dk) { return Dk > 128 ? 13 : 7; }
 
 // Pieces of long sequences.  Computing the states at the seams costs about 0.4 of the forward itself, so sequences are
 // cut only until every compute unit has eight waves; twice as many pieces, half as long, pay only where a piece still has many
