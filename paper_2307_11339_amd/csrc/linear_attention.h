@@ -13,6 +13,17 @@ struct LaView {                // a [T, B, heads, size] tensor: strides in eleme
     int64_t t, b, h;
 };
 
+struct LaDivide {              // n / d for n < 2^31 by one product: for d <= 2^l, n (2^(31 + l) / d + 1) >> (31 + l)
+    uint32_t by, shift;
+    void set(uint32_t d) {
+        uint32_t l = 0;
+        while (((uint64_t)1 << l) < d) ++l;
+        shift = 31 + l;
+        by = (uint32_t)(((uint64_t)1 << shift) / d + 1);
+    }
+    __device__ inline uint32_t of(uint32_t n) const { return (uint32_t)(((uint64_t)n * by) >> shift); }
+};
+
 struct LaArgs {
     const void* q;
     const void* k;
@@ -28,10 +39,11 @@ struct LaArgs {
                                // [pieces, B, H, vblocks][wave][block of 16 rows][lane][4]: rows 4 (lane / 16) + 0..3 of a block,
                                // column lane % 16 of the wave's sixteen
     float scale;
-    int T, B, H, rep;          // rep: heads that share a head of k and v
+    int T, B, H, Hkv, rep;     // rep: heads that share a head of k and v
     int Dk, Dv;
     int vblocks, columns;      // workgroups that share the Dv columns of one state, columns of each but the last
     int pieces, piece_steps;   // pieces of a sequence along time; steps of one (a multiple of LA_CHUNK when pieces > 1)
+    LaDivide by_shared, by_pieces, by_kv, by_vblocks;      // of a launch of chunks, see la_place
 };
 
 // linear_attention.hip: one step after the other, for short calls.  wide: 128 columns a workgroup instead of 32.
@@ -90,13 +102,13 @@ __device__ inline int la_sequence_of_rank(const LaArgs& a, int rank) {
 }
 
 __device__ inline bool la_place(const LaArgs& a, int pieces, LaPlace* p) {
-    // at most 2^22 workgroups with work: 32-bit divisions
-    const uint32_t kv = a.H / a.rep, units = (uint32_t)a.B * kv * pieces, shared = a.rep * a.vblocks;
-    const uint32_t idx = blockIdx.x / 8, turn = idx / shared, unit = turn * 8 + blockIdx.x % 8;
+    // at most 2^22 workgroups with work: 32 bits are enough
+    const uint32_t kv = a.Hkv, units = (uint32_t)a.B * kv * pieces, shared = a.rep * a.vblocks;
+    const uint32_t idx = blockIdx.x / 8, turn = a.by_shared.of(idx), unit = turn * 8 + blockIdx.x % 8;
     if (unit >= units) return false;
-    const uint32_t r = idx - turn * shared, seq = unit / pieces, head = r / a.vblocks;
+    const uint32_t r = idx - turn * shared, seq = a.by_pieces.of(unit), head = a.by_vblocks.of(r);
     p->piece = (int)(unit - seq * pieces);
-    p->b = (int)(seq / kv);
+    p->b = (int)a.by_kv.of(seq);
     p->hk = (int)(seq - p->b * kv);
     p->b = la_sequence_of_rank(a, p->b);
     p->h = (int)(p->hk * a.rep + head);
@@ -108,8 +120,14 @@ __device__ inline bool la_place(const LaArgs& a, int pieces, LaPlace* p) {
     return true;
 }
 
-inline int64_t la_grid(const LaArgs& a, int pieces) {
-    const int64_t units = (int64_t)a.B * (a.H / a.rep) * pieces;
+// Workgroups of a launch; sets what la_place divides by.
+inline int64_t la_grid(LaArgs* args, int pieces) {
+    LaArgs& a = *args;
+    a.by_shared.set(a.rep * a.vblocks);
+    a.by_pieces.set(pieces);
+    a.by_kv.set(a.Hkv);
+    a.by_vblocks.set(a.vblocks);
+    const int64_t units = (int64_t)a.B * a.Hkv * pieces;
     return (units + 7) / 8 * 8 * a.rep * a.vblocks;
 }
 

@@ -456,7 +456,7 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
     a.lengths = lengths; a.s0 = s0; a.sT = sT;
     a.powers = l->powers; a.log2_decay = l->log2_decay; a.seams = l->seams;
     a.scale = l->scale;
-    a.T = T; a.B = B; a.H = l->H; a.rep = l->H / l->Hkv; a.Dk = l->Dk; a.Dv = l->Dv;
+    a.T = T; a.B = B; a.H = l->H; a.Hkv = l->Hkv; a.rep = l->H / l->Hkv; a.Dk = l->Dk; a.Dv = l->Dv;
     a.vblocks = p.vblocks; a.columns = p.columns; a.pieces = p.pieces; a.piece_steps = p.piece_steps;
     hipError_t e = hipSuccess;
     if (!p.chunk) {

@@ -366,8 +366,8 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
 }
 
 template <bool STATES>
-bool launch(const LaArgs& a, int kt, int nw, hipStream_t stream) {
-    const unsigned grid = (unsigned)la_grid(a, STATES ? a.pieces - 1 : a.pieces);
+bool launch(LaArgs a, int kt, int nw, hipStream_t stream) {
+    const unsigned grid = (unsigned)la_grid(&a, STATES ? a.pieces - 1 : a.pieces);
 #define LA_CHUNK_CASE(K, N) \
     if (kt == K && nw == N) { la_chunk_kernel<K, N, STATES><<<grid, 64 * N, 0, stream>>>(a); return true; }
     LA_CHUNK_CASE(1, 2) LA_CHUNK_CASE(1, 4) LA_CHUNK_CASE(1, 8)
