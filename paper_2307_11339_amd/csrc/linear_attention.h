@@ -43,7 +43,9 @@ struct LaArgs {
     int Dk, Dv;
     int vblocks, columns;      // workgroups that share the Dv columns of one state, columns of each but the last
     int pieces, piece_steps;   // pieces of a sequence along time; steps of one (a multiple of LA_CHUNK when pieces > 1)
-    LaDivide by_shared, by_pieces, by_kv, by_vblocks;      // of a launch of chunks, see la_place
+    LaDivide by_vblocks;       // set by what launches a kernel, and for chunks (la_place)
+    LaDivide by_shared, by_pieces, by_kv;
+    LaDivide by_heads, by_rep; // for steps
 };
 
 // linear_attention.hip: one step after the other, for short calls.  wide: 128 columns a workgroup instead of 32.

@@ -59,9 +59,9 @@ __global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) 
 
     const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
     const int col = (tid % LANES) * 4, group = tid / LANES;
-    const int64_t unit = blockIdx.x / a.vblocks;       // (sequence, head)
-    const int v0 = (int)(blockIdx.x % a.vblocks) * COLS;
-    const int b = (int)(unit / a.H), h = (int)(unit % a.H), hk = h / a.rep;
+    const uint32_t unit = a.by_vblocks.of(blockIdx.x);           // (sequence, head)
+    const int v0 = (int)(blockIdx.x - unit * a.vblocks) * COLS;
+    const int b = (int)a.by_heads.of(unit), h = (int)(unit - b * a.H), hk = (int)a.by_rep.of(h);
     const int cols = min(COLS, a.Dv - v0);             // a multiple of 4
     const bool mine = col < cols;
     const float decay = a.powers[h * (LA_CHUNK + 1) + 1];
@@ -74,7 +74,8 @@ __global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) 
     T* o = (T*)a.o + b * a.os.b + h * a.os.h + v0;
 
     float4 S[ROWS];
-    const float* s0 = a.s0 ? a.s0 + (unit * a.Dk) * a.Dv + v0 + col : nullptr;
+    const int64_t state_at = (int64_t)unit * a.Dk * a.Dv + v0 + col;
+    const float* s0 = a.s0 ? a.s0 + state_at : nullptr;
 #pragma unroll
     for (int r = 0; r < ROWS; ++r) {
         const int row = r * GROUPS + group;
@@ -82,24 +83,21 @@ __global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) 
         if (s0 && mine && row < a.Dk) S[r] = *reinterpret_cast<const float4*>(s0 + (int64_t)row * a.Dv);
     }
 
-    constexpr int N = Vec16<T>::N;
-    const int kc = a.Dk / N, vc = cols / N;            // 16-byte pieces of a row
+    constexpr int N = Vec16<T>::N, KC = DK / N, PIECES = 2 * KC + COLS / N;      // 16-byte pieces of a step: of q, of k, of v
     for (int t0 = 0; t0 < len; t0 += STEP_BLOCK) {
         const int n = min(STEP_BLOCK, len - t0);
         if (t0) __syncthreads();                       // the block before is used up
-        for (int i = tid; i < n * kc; i += STEP_THREADS) {
-            const int s = i / kc, c = (i % kc) * N;
-            Vec16<T>::load(q + (t0 + s) * a.qs.t + c, &sq[s][c]);
-            Vec16<T>::load(k + (t0 + s) * a.ks.t + c, &sk[s][c]);
-        }
-        for (int i = tid; i < n * (DK - a.Dk); i += STEP_THREADS) {      // rows that no element of the tensors has
-            const int s = i / (DK - a.Dk), c = a.Dk + i % (DK - a.Dk);
-            sq[s][c] = 0.f;
-            sk[s][c] = 0.f;
-        }
-        for (int i = tid; i < n * vc; i += STEP_THREADS) {
-            const int s = i / vc, c = (i % vc) * N;
-            Vec16<T>::load(v + (t0 + s) * a.vs.t + c, &sv[s][c]);
+        // all three in one loop: one way to memory for a step or a few
+        for (int i = tid; i < n * PIECES; i += STEP_THREADS) {
+            const int s = i / PIECES, piece = i % PIECES, c = (piece < 2 * KC ? piece % KC : piece - 2 * KC) * N;
+            const T* row = piece < KC ? q + (t0 + s) * a.qs.t : piece < 2 * KC ? k + (t0 + s) * a.ks.t : v + (t0 + s) * a.vs.t;
+            float* to = piece < KC ? &sq[s][c] : piece < 2 * KC ? &sk[s][c] : &sv[s][c];
+            if (c < (piece < 2 * KC ? a.Dk : cols)) {
+                Vec16<T>::load(row + c, to);
+            } else if (piece < 2 * KC) {               // rows that no element of the tensors has
+#pragma unroll
+                for (int e = 0; e < N; ++e) to[e] = 0.f;
+            }
         }
         __syncthreads();
         for (int s = 0; s < n; ++s) {
@@ -123,8 +121,9 @@ __global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) 
             if (lane < LANES) *reinterpret_cast<float4*>(&part[s][wave][col]) = acc;
         }
         __syncthreads();
-        for (int i = tid; i < n * cols; i += STEP_THREADS) {
-            const int s = i / cols, c = i % cols;
+        for (int i = tid; i < n * COLS; i += STEP_THREADS) {
+            const int s = i / COLS, c = i % COLS;
+            if (c >= cols) continue;
             float sum = part[s][0][c];
 #pragma unroll
             for (int w = 1; w < WAVES; ++w) sum += part[s][w][c];
@@ -134,7 +133,7 @@ __global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) 
     for (int64_t i = tid; i < (int64_t)(a.T - len) * cols; i += STEP_THREADS)
         store_one(o + (len + i / cols) * a.os.t + i % cols, 0.f);
     if (a.sT && mine) {
-        float* sT = a.sT + (unit * a.Dk) * a.Dv + v0 + col;
+        float* sT = a.sT + state_at;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r) {
             const int row = r * GROUPS + group;
@@ -144,7 +143,10 @@ __global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) 
 }
 
 template <typename T>
-void launch_steps(const LaArgs& a, bool wide, hipStream_t stream) {
+void launch_steps(LaArgs a, bool wide, hipStream_t stream) {
+    a.by_vblocks.set(a.vblocks);
+    a.by_heads.set(a.H);
+    a.by_rep.set(a.rep);
     const dim3 grid((unsigned)((int64_t)a.B * a.H * a.vblocks));
 #define LA_STEPS(C, R) la_steps_kernel<T, C, R><<<grid, STEP_THREADS, 0, stream>>>(a)
     if (wide) {
