@@ -219,9 +219,9 @@ inline int fewest_steps(int Dk) { return Dk > 128 ? 13 : 7; }
 
 // Pieces of long sequences.  Computing the states at the seams costs about 0.4 of the forward itself, so sequences are
 // cut only until every compute unit has eight waves; twice as many pieces, half as long, pay only where a piece still has many
-// steps.  16 heads of 128: 2048 steps of 16 sequences 160 us whole, 197 in two pieces; 65536 steps of one
-// 371 us in 32 pieces, 408 in 16; 4096 steps 49 us in 16 pieces, 57 in 32, 64 in 8; 16 sequences of 512 steps, 8 fp32 heads of
-// 64: 43 us in 4 pieces, 47 in 2 or 8, 52 whole.
+// steps.  16 heads of 128: 2048 steps of 16 sequences 155 us whole, 190 in two pieces; 65536 steps of one
+// 371 us in 32 pieces, 406 in 16; 4096 steps 49 us in 16 pieces, 57 in 32, 62 in 8; 16 sequences of 512 steps, 8 fp32 heads of
+// 64: 42 us in 4 pieces, 46 in 2, 45 in 8.
 constexpr int LA_WAVES = 2048, LA_LONG_WAVES = 4096;       // eight a compute unit; sixteen
 constexpr int LA_LONG_STEPS = 1024;
 constexpr int LA_PIECE_STEPS = 128;                // of a piece at least
