@@ -537,3 +537,51 @@ def test_without_initial_state_or_new_state(gpu, dtype):
         c.sT, c.s0 = sT, None
         assert c.forward() == rnn.RNN_OK
         c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,H,Hkv,B", [(1, 65535, 65535, 1), (9, 65535, 1, 1), (9, 4369, 257, 3), (2, 12, 4, 511)])
+def test_many_heads(gpu, T, H, Hkv, B, dtype):
+    c = Case(T, B, H, Hkv, 8, 8, dtype, lengths=None if B == 1 else [T - b % 2 for b in range(B)])
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_two_graphs_of_a_layer_in_turn(gpu, dtype):
+    """Two recorded calls of different lengths share the layer's workspace; replayed one after the other, with eager calls
+    between them, each gives what it gave alone."""
+    torch = gpu
+    long = Case(2100, 1, 2, 1, 64, 64, dtype)
+    short = Case(1300, 2, 2, 1, 64, 64, dtype, lengths=[1300, 700])
+    rnn.rnn_linear_attention_destroy(short.handle)
+    short.handle = None
+
+    def call(c, stream):
+        return rnn.rnn_linear_attention_forward(long.handle, c.q, c.k, c.v, c.lengths, c.s0, c.o, c.sT, c.T, c.B, stream)
+
+    s, graphs, want = torch.cuda.Stream(), [], []
+    s.wait_stream(torch.cuda.current_stream())
+    for c in (long, short):
+        assert rnn.rnn_linear_attention_plan_query(2, 1, 64, 64, dtype, c.T, c.B)[1]["pieces"] > 1
+        assert call(c, s) == rnn.RNN_OK
+        torch.cuda.synchronize()
+        c.check()
+        want.append((c.o.clone(), c.sT.clone()))
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1], stream=s):
+            assert call(c, s) == rnn.RNN_OK
+    for r in range(3):
+        for i, c in enumerate((long, short)):
+            c.o.fill_(7.0)
+            c.sT.fill_(7.0)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(s):
+                graphs[i].replay()
+                if r == 1:
+                    assert call((short, long)[i], s) == rnn.RNN_OK
+            torch.cuda.synchronize()
+            assert torch.equal(c.o, want[i][0]) and torch.equal(c.sT, want[i][1])
+    del graphs
