@@ -35,14 +35,15 @@ struct LaArgs {
     float* sT;                 // likewise; may be s0
     const float* powers;       // [H, LA_CHUNK + 1]: decay[h]^n
     const double* log2_decay;  // [H]
-    float* seams;              // when pieces > 1: the state that each piece starts from, as the chunk kernels hold it
-                               // [pieces, B, H, vblocks][wave][block of 16 rows][lane][4]: rows 4 (lane / 16) + 0..3 of a block,
-                               // column lane % 16 of the wave's sixteen
+    float* seams;              // when pieces > 1, [pieces, B, H, vblocks][wave][block of 16 rows][lane][4], as the chunk kernels hold a
+                               // state: 0 a copy of s0, 1 the state behind the first piece, x > 1 what piece x - 1 adds, or when
+                               // joined the state behind it
     float scale;
     int T, B, H, Hkv, rep;     // rep: heads that share a head of k and v
     int Dk, Dv;
     int vblocks, columns;      // workgroups that share the Dv columns of one state, columns of each but the last
     int pieces, piece_steps;   // pieces of a sequence along time; steps of one (a multiple of LA_CHUNK when pieces > 1)
+    bool joined;
     LaDivide by_vblocks;       // set by what launches a kernel, and for chunks (la_place)
     LaDivide by_shared, by_pieces, by_kv;
     LaDivide by_heads, by_rep; // for steps
@@ -138,6 +139,14 @@ inline int64_t la_grid(LaArgs* args, int pieces) {
     a.by_vblocks.set(a.vblocks);
     const int64_t units = (int64_t)a.B * a.Hkv * pieces;
     return (units + 7) / 8 * 8 * a.rep * a.vblocks;
+}
+
+// decay^n from its logarithm, which is 0 or less: to fp32's rounding whatever n
+__device__ inline float la_power(double log2_decay, int n) {
+    const double y = n * log2_decay;
+    if (!(y > -160.0)) return 0.f;
+    const double whole = floor(y);
+    return ldexpf(exp2f((float)(y - whole)), (int)whole);
 }
 
 // Tiles in LDS: rows of ROW bytes (64 to 1024), whose pieces of 16 bytes change places from row to row, so that the ways of

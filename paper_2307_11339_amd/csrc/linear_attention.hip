@@ -175,28 +175,19 @@ namespace {
 
 // The pieces of sequences know what they add to the state; this turns it into the state that each starts from.
 // One thread for four numbers of a state, as the seams hold them; bound by reading and writing the seams once.
-__global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a, int key_tiles, int waves, bool bf16) {
-    const int64_t per = la_seam(key_tiles, waves), all = (int64_t)a.B * a.H * a.vblocks * per;
+__global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a, int64_t per) {
+    const int64_t all = (int64_t)a.B * a.H * a.vblocks * per;
     const int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (i >= all) return;
-    const uint32_t block = (uint32_t)(i / per), in = (uint32_t)(i - block * per);
-    const uint32_t unit = block / a.vblocks, b = unit / a.H, h = unit - b * a.H;
+    const uint32_t block = (uint32_t)(i / per), unit = block / a.vblocks, b = unit / a.H, h = unit - b * a.H;
     const int len = min(a.lengths ? a.lengths[b] : a.T, a.T);
-    const float decay = (float)exp2((double)a.piece_steps * a.log2_decay[h]);
-    f32x4 run = {0.f, 0.f, 0.f, 0.f};
-    if (a.s0) {
-        const int lane = in >> 2 & 63, y = (in >> 8) % (2 * key_tiles), wave = (in >> 8) / (2 * key_tiles);
-        const int col = (int)(block - unit * a.vblocks) * a.columns + wave * 16 + (lane & 15);
-        const int row = bf16 ? 32 * (y >> 1) + 8 * (lane >> 4) + 4 * (y & 1) : 16 * y + 4 * (lane >> 4);
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (wave * 16 < a.columns && col < a.Dv && row + e < a.Dk) run[e] = a.s0[((int64_t)unit * a.Dk + row + e) * a.Dv + col];
-        *reinterpret_cast<f32x4*>(a.seams + i) = run;    // the first piece reads it here: sT may be s0
-    }
+    const float decay = la_power(a.log2_decay[h], a.piece_steps);
     int live = 1;                                      // pieces that have steps to start
     while (live < a.pieces && len > live * a.piece_steps) ++live;
+    if (live <= 2) return;
+    f32x4 run = *reinterpret_cast<const f32x4*>(a.seams + all + i);
     constexpr int AT_ONCE = 8;                         // loads under way together: the sum is short, the way to memory long
-    for (int p0 = 1; p0 < live; p0 += AT_ONCE) {
+    for (int p0 = 2; p0 < live; p0 += AT_ONCE) {
         f32x4 add[AT_ONCE];
 #pragma unroll
         for (int j = 0; j < AT_ONCE; ++j) add[j] = *reinterpret_cast<const f32x4*>(a.seams + min(p0 + j, live - 1) * all + i);
@@ -221,10 +212,14 @@ inline int fewest_steps(int Dk) { return Dk > 128 ? 13 : 7; }
 // cut only until every compute unit has eight waves; twice as many pieces, half as long, pay only where a piece still has many
 // steps.  16 heads of 128: 2048 steps of 16 sequences 155 us whole, 190 in two pieces; 65536 steps of one
 // 371 us in 32 pieces, 406 in 16; 4096 steps 49 us in 16 pieces, 57 in 32, 62 in 8; 16 sequences of 512 steps, 8 fp32 heads of
-// 64: 42 us in 4 pieces, 46 in 2, 45 in 8.
+// 64, all joined by a launch, 42 us in 4 pieces, 46 in 2, 45 in 8.
 constexpr int LA_WAVES = 2048, LA_LONG_WAVES = 4096;       // eight a compute unit; sixteen
 constexpr int LA_LONG_STEPS = 1024;
 constexpr int LA_PIECE_STEPS = 128;                // of a piece at least
+// Up to so many pieces each adds up by itself what those before it add; more are joined by a launch in between, as the last one
+// would have much to read.  16 sequences of 512 steps, 8 heads of 64: four pieces 24.1 us, joined 26.0 (fp32 39.2 and 41.2); 1024 steps
+// of one, 16 heads of 64: eight pieces 19.1, joined 18.6; 4096 steps, 16 heads of 128: sixteen 55.7, joined 48.7.
+constexpr int LA_CHAINED_PIECES = 4;
 
 struct LaPlan {
     int chunk = 0, vblocks = 1, columns = 0, pieces = 1, piece_steps = 0;
@@ -462,6 +457,7 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
     a.scale = l->scale;
     a.T = T; a.B = B; a.H = l->H; a.Hkv = l->Hkv; a.rep = l->H / l->Hkv; a.Dk = l->Dk; a.Dv = l->Dv;
     a.vblocks = p.vblocks; a.columns = p.columns; a.pieces = p.pieces; a.piece_steps = p.piece_steps;
+    a.joined = p.pieces > LA_CHAINED_PIECES;
     hipError_t e = hipSuccess;
     if (!p.chunk) {
         e = la_launch_steps(l->dtype, a, p.wide, st);
@@ -470,9 +466,9 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
         const int kt = la_key_tiles(l->Dk), nw = la_waves(l->Dk, l->Dv);
         if (p.pieces > 1) {
             e = chunks(a, kt, nw, true, st);
-            if (e == hipSuccess) {
+            if (e == hipSuccess && a.joined) {
                 const int64_t quads = (int64_t)B * l->H * p.vblocks * la_seam(kt, nw) / 4;     // few: pieces are cut where heads are
-                la_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a, kt, nw, l->dtype == RNN_BF16);
+                la_join_kernel<<<(unsigned)((quads + 255) / 256), 256, 0, st>>>(a, la_seam(kt, nw));
                 e = hipGetLastError();
             }
         }

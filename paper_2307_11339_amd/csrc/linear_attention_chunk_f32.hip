@@ -91,11 +91,30 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                (wave * 2 * KT) * 64 + lane;
     };
     f32x4 S[2 * KT];
-    if (!STATES && live > 0 && (at.piece > 0 || (a.pieces > 1 && a.s0))) {
-        const f32x4* from = seam(at.piece);
+    // sT may be s0, which the sequence's last piece writes when it likes: a first piece with others behind it has a copy in the seams
+    if (!STATES && live > 0 && (at.piece > 0 || (a.s0 && at.len > at.t1))) {
+        const f32x4* from = seam(a.joined ? at.piece : min(at.piece, 1));
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y) S[y] = from[y * 64];
-    } else if (!STATES && a.s0 && at.piece == 0) {
+        if (!a.joined && at.piece > 1) {               // what the pieces before this one add
+            const float decay = la_power(a.log2_decay[at.h], a.piece_steps);
+            constexpr int AT_ONCE = KT <= 4 ? 2 : 1;   // as registers allow: loads under way together
+#pragma unroll 1
+            for (int p = 2; p <= at.piece; p += AT_ONCE) {
+                f32x4 add[AT_ONCE][2 * KT];
+#pragma unroll
+                for (int j = 0; j < AT_ONCE; ++j)
+#pragma unroll
+                    for (int y = 0; y < 2 * KT; ++y) add[j][y] = seam(min(p + j, at.piece))[y * 64];
+#pragma unroll
+                for (int j = 0; j < AT_ONCE; ++j)
+                    if (p + j <= at.piece) {
+#pragma unroll
+                        for (int y = 0; y < 2 * KT; ++y) S[y] = decay * S[y] + add[j][y];
+                    }
+            }
+        }
+    } else if (a.s0 && at.piece == 0) {
         const __amdgpu_buffer_rsrc_t rows = la_rows(a.s0 + state_at, 4 * a.Dv, cols, a.Dk);
         const uint32_t first = my_col < cols ? (uint32_t)(4 * g * a.Dv + my_col) * 4 : 0x80000000u;
 #pragma unroll
@@ -110,6 +129,11 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
     // the state is waited for here: inside the loop the wait would be for the outputs of the chunk before as well
 #pragma unroll
     for (int y = 0; y < 2 * KT; ++y) asm volatile("" : "+v"(S[y]));
+    if (STATES && a.s0 && at.piece == 0) {
+        f32x4* to = seam(0);
+#pragma unroll
+        for (int y = 0; y < 2 * KT; ++y) to[y * 64] = S[y];
+    }
     if (tid <= C) {
         power[tid] = my_power;
         scaled[tid] = my_power * a.scale;
@@ -192,12 +216,14 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                 for (int e = 0; e < 4; ++e) wv[e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
                 wv *= *reinterpret_cast<const f32x4*>(weight + 16 * s + 4 * g);
 #pragma unroll
-                for (int y = 0; y < 2 * KT; y += 2)
+                for (int y = 0; y < 2 * KT; y += 2) {
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
 #pragma unroll
                         for (int z = 0; z < 2; ++z)
                             S[y + z] = mma(*reinterpret_cast<const float*>(sk + 16 * s * KR + la_block(k_at[e], y + z)), wv[e], S[y + z]);
+                    if (KT >= 4 && y % 4 == 2) __builtin_amdgcn_sched_barrier(0);
+                }
                 __builtin_amdgcn_sched_barrier(0);      // operands of one half at a time: there are no registers for both
             }
             if (!STATES) {
