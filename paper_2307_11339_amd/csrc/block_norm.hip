@@ -8,8 +8,7 @@
 // Layout.  A row is a line of slots, one piece of 16 bytes each (or three of one group); thread i of the row's `waves`
 // waves holds slots i, i + 64 waves, .. (VPT pieces in all).  A group starts a power of two of slots, or a whole number of 64, so that 64 neighbouring
 // slots, which a wave sums up with cross-lane instructions, hold whole groups or belong to one.  Rows of one wave need
-// no barrier: 65536 rows of 2048 bf16 values, sum and norm, take 204 us with one wave of four pieces a thread, 219 us with
-// two waves and a barrier for the sum.
+// no barrier, rows of more waves one for every sum.
 // The parts that a norm lacks are compiled out (AFTER, GATE, BEFORE).
 #include "../../include/rnn.h"
 #include "common.h"
@@ -388,16 +387,17 @@ bool norm_slots(int width, int groups, int vec, NormLayout* out) {
 
 // How `rows` rows are divided.  Rows that are few are spread over as many waves as they have pieces for, until there is
 // a wave for every SIMD of the GPU (64 rows of 1024 bf16 values: 3.7 us with one piece a thread, 4.3 with two, 5.1 with four).
-// Many rows take as few waves each as hold four pieces a thread (five of fp32), and three with a norm by groups, whose
-// registers would leave too few waves a SIMD (17157 padded rows of 1280 fp32 values, everything at once: 98 us with
-// three, 110 with five; 65536 rows of 16 gated heads of 128: 168 with two, 181 with four).
-void norm_divide(NormLayout* l, int64_t rows, int vec, bool after, int simds) {
+// Many rows take as few waves each as hold two pieces a thread: more pieces leave too few waves a SIMD, fewer cost barriers.
+// 65536 rows of 2048 bf16 values, sum and norm: 201 us with two, 206 with four (and no barrier) or one; 17157 padded rows of 1280 fp32
+// values, everything at once: 92 with two or three, 103 with one, 110 with five; 16384 rows of 16 gated fp32 heads of 128: 80 with
+// two, 90 with three; 65536 of bf16 ones 158 with two, 176 with four.  (32768 rows of 8192: 400 with two, 392 with four.)
+void norm_divide(NormLayout* l, int64_t rows, int simds) {
     if (l->slots <= 32 && (l->slots & (l->slots - 1)) == 0 && l->deep == 1) {
         l->waves = l->vpt = 1;
         l->rows = 256 / l->slots;
         return;
     }
-    const int chunks = (l->slots + 63) / 64, most = after ? 3 / l->deep : vec == 4 ? 5 : 4;
+    const int chunks = (l->slots + 63) / 64, most = l->deep == 3 ? 1 : 2;
     int w = (chunks + most - 1) / most;
     while (w < chunks && w < NORM_WAVES && rows * w < simds) ++w;
     if (w > NORM_WAVES) w = NORM_WAVES;
@@ -570,10 +570,12 @@ int rnn_block_norm_forward(const rnn_block_norm* n, const void* x, const int64_t
     a.shift = 31 + l;
     a.divide = (uint32_t)(((uint64_t)1 << a.shift) / a.inner + 1);
     const int64_t rows = (int64_t)T * B;
-    norm_divide(&a.lay, rows, step, n->after != RNN_NORM_NONE, 4 * n->cus);
+    norm_divide(&a.lay, rows, 4 * n->cus);
     const int64_t wgs = (rows + a.lay.rows - 1) / a.lay.rows;
     const unsigned threads = a.lay.rows > 4 ? 256 : 64 * a.lay.waves * a.lay.rows;
-    const int64_t most = (int64_t)n->cus * 2048 / threads;             // what the GPU holds at once
+    // Four times what the GPU holds at once: workgroups of a few rows each take what has become free.  131072 rows of 1024 bf16 values
+    // 199 us, 213 with as many as it holds and 195 with one row a wave; but 65536 rows of 16 gated heads 158, 167 and 172.
+    const int64_t most = (int64_t)n->cus * 8192 / threads;
     const unsigned grid = (unsigned)(wgs < most ? wgs : most);
     if (n->dtype == RNN_BF16) launch_norm<bf16_t>(a, grid, threads, (hipStream_t)stream);
     else launch_norm<float>(a, grid, threads, (hipStream_t)stream);
