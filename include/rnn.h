@@ -417,7 +417,8 @@ int rnn_linear_attention_reserve(rnn_linear_attention* layer, int T, int B);
  * Stream capture: may be recorded into a HIP graph; RNN_EUNSUPPORTED, with nothing recorded, if the workspace would have to be
  * allocated first.  One forward in flight per layer (a replay counts), as the workspace is the layer's.
  * RNN_EINVAL if the layer belongs to another device than the current one.  RNN_EUNSUPPORTED if T * B > 2^30 or
- * B * H * (workgroups that share a state) * (pieces of a sequence) > 2^22 (see rnn_linear_attention_plan_query).
+ * B * H * (workgroups that share a state) * (pieces of a sequence) > 2^22 (see rnn_linear_attention_plan_query;
+ * 32 columns a workgroup for tensors that go one step after the other).
  */
 int rnn_linear_attention_forward(rnn_linear_attention* layer, const void* q, const int64_t* q_strides, const void* k,
                                  const int64_t* k_strides, const void* v, const int64_t* v_strides,

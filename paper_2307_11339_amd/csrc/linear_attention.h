@@ -49,8 +49,8 @@ struct LaArgs {
     LaDivide by_heads, by_rep; // for steps
 };
 
-// linear_attention.hip: one step after the other, for short calls.  wide: 128 columns a workgroup instead of 32.
-hipError_t la_launch_steps(int dtype, const LaArgs& a, bool wide, hipStream_t stream);
+// linear_attention.hip: one step after the other, for short calls.
+hipError_t la_launch_steps(int dtype, const LaArgs& a, hipStream_t stream);
 
 // linear_attention_chunk.hip, linear_attention_chunk_f32.hip: chunks of steps by matrix products.  key_tiles, waves: from
 // la_key_tiles and la_waves.  With `states` only the state that each piece but the last adds is computed, into the seams.

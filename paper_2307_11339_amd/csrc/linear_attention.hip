@@ -20,9 +20,9 @@ namespace {
 
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-// Steps whose q, k and v are staged in LDS together.  With sixteen, LDS holds two wide workgroups a compute unit instead of four: four
-// steps of 128 sequences, 16 heads of 128, 62 us against 58; twelve of 4 sequences, 4 heads of 256, 11.3 against 11.7.
-constexpr int STEP_BLOCK = 8;
+// Columns of a state that a workgroup takes, and steps whose q, k and v are staged in LDS together: small, for many waves
+// on a compute unit.  With 128 columns one step of 128 sequences, 16 heads of 128, takes 56 us, with 32 52; six steps 63 and 57.
+constexpr int STEP_COLS = 32, STEP_BLOCK = 8;
 constexpr int STEP_THREADS = 256;
 
 template <typename T> struct Vec16;            // 16 bytes of the storage type
@@ -49,10 +49,10 @@ template <> struct Vec16<bf16_t> {
 __device__ inline void store_one(float* p, float v) { *p = v; }
 __device__ inline void store_one(bf16_t* p, float v) { *reinterpret_cast<__bf16*>(p) = (__bf16)v; }
 
-// COLS columns of one state a workgroup, four neighbouring ones a thread; ROWS rows a thread, GROUPS apart.
-template <typename T, int COLS, int ROWS>
+// Four neighbouring columns of a state a thread; ROWS rows a thread, GROUPS apart.
+template <typename T, int ROWS>
 __global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) {
-    constexpr int LANES = COLS / 4;                    // lanes that hold one row
+    constexpr int COLS = STEP_COLS, LANES = COLS / 4;                    // lanes that hold one row
     constexpr int GROUPS = STEP_THREADS / LANES;       // rows held side by side
     constexpr int WAVES = STEP_THREADS / 64;
     constexpr int DK = GROUPS * ROWS;                  // at least Dk; rows behind Dk stay zero
@@ -145,29 +145,22 @@ __global__ __launch_bounds__(STEP_THREADS) void la_steps_kernel(const LaArgs a) 
 }
 
 template <typename T>
-void launch_steps(LaArgs a, bool wide, hipStream_t stream) {
+void launch_steps(LaArgs a, hipStream_t stream) {
     a.by_vblocks.set(a.vblocks);
     a.by_heads.set(a.H);
     a.by_rep.set(a.rep);
-    const dim3 grid((unsigned)((int64_t)a.B * a.H * a.vblocks));
-#define LA_STEPS(C, R) la_steps_kernel<T, C, R><<<grid, STEP_THREADS, 0, stream>>>(a)
-    if (wide) {
-        if (a.Dk <= 64) LA_STEPS(128, 8);
-        else if (a.Dk <= 128) LA_STEPS(128, 16);
-        else LA_STEPS(128, 32);
-    } else {
-        if (a.Dk <= 64) LA_STEPS(32, 2);
-        else if (a.Dk <= 128) LA_STEPS(32, 4);
-        else LA_STEPS(32, 8);
-    }
-#undef LA_STEPS
+    const unsigned grid = (unsigned)((int64_t)a.B * a.H * a.vblocks);
+    constexpr int GROUPS = STEP_THREADS / (STEP_COLS / 4);
+    if (a.Dk <= 64) la_steps_kernel<T, 64 / GROUPS><<<grid, STEP_THREADS, 0, stream>>>(a);
+    else if (a.Dk <= 128) la_steps_kernel<T, 128 / GROUPS><<<grid, STEP_THREADS, 0, stream>>>(a);
+    else la_steps_kernel<T, 256 / GROUPS><<<grid, STEP_THREADS, 0, stream>>>(a);
 }
 
 }  // namespace
 
-hipError_t la_launch_steps(int dtype, const LaArgs& a, bool wide, hipStream_t stream) {
-    if (dtype == DT_BF16) launch_steps<bf16_t>(a, wide, stream);
-    else launch_steps<float>(a, wide, stream);
+hipError_t la_launch_steps(int dtype, const LaArgs& a, hipStream_t stream) {
+    if (dtype == DT_BF16) launch_steps<bf16_t>(a, stream);
+    else launch_steps<float>(a, stream);
     return hipGetLastError();
 }
 
@@ -223,20 +216,18 @@ constexpr int LA_CHAINED_PIECES = 4;
 
 struct LaPlan {
     int chunk = 0, vblocks = 1, columns = 0, pieces = 1, piece_steps = 0;
-    bool wide = false;
 };
 
-LaPlan steps_plan(int H, int Dv, int T, int B) {
+LaPlan steps_plan(int Dv, int T) {
     LaPlan p;
     p.piece_steps = T;
-    p.wide = (int64_t)B * H * ((Dv + 127) / 128) >= 512;
-    p.columns = p.wide ? 128 : 32;
+    p.columns = STEP_COLS;
     p.vblocks = (Dv + p.columns - 1) / p.columns;
     return p;
 }
 
 LaPlan choose(int H, int Dk, int Dv, int dtype, int T, int B) {
-    if (T < fewest_steps(Dk)) return steps_plan(H, Dv, T, B);
+    if (T < fewest_steps(Dk)) return steps_plan(Dv, T);
     LaPlan p;
     p.piece_steps = T;
     p.chunk = dtype == RNN_BF16 ? LA_CHUNK : LA_CHUNK_F32;
@@ -423,7 +414,7 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o | (uintptr_t)s0 | (uintptr_t)sT) & 15) return RNN_EINVAL;
     if ((uintptr_t)lengths & 3) return RNN_EINVAL;
     LaPlan p = choose(l->H, l->Dk, l->Dv, l->dtype, T, B);
-    const int rc = check_call(l->H, T, B, p);
+    int rc = check_call(l->H, T, B, p);
     if (rc != RNN_OK) return rc;
     const int step = l->dtype == RNN_BF16 ? 8 : 4;
     LaArgs a = {};
@@ -432,8 +423,11 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
         !rows_apart(a.os, T, B, l->H, l->Dv))
         return RNN_EINVAL;
     if (p.chunk && !(chunk_rows(a.qs, T, l->Dk, l->dtype) && chunk_rows(a.ks, T, l->Dk, l->dtype) && chunk_rows(a.vs, T, l->Dv, l->dtype) &&
-                     chunk_rows(a.os, T, l->Dv, l->dtype)))
-        p = steps_plan(l->H, l->Dv, T, B);
+                     chunk_rows(a.os, T, l->Dv, l->dtype))) {
+        p = steps_plan(l->Dv, T);
+        rc = check_call(l->H, T, B, p);
+        if (rc != RNN_OK) return rc;
+    }
     int device = -1;
     if (hipGetDevice(&device) != hipSuccess) {
         (void)hipGetLastError();
@@ -460,7 +454,7 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
     a.joined = p.pieces > LA_CHAINED_PIECES;
     hipError_t e = hipSuccess;
     if (!p.chunk) {
-        e = la_launch_steps(l->dtype, a, p.wide, st);
+        e = la_launch_steps(l->dtype, a, st);
     } else {
         const auto chunks = l->dtype == RNN_BF16 ? la_launch_chunks_bf16 : la_launch_chunks_f32;
         const int kt = la_key_tiles(l->Dk), nw = la_waves(l->Dk, l->Dv);
