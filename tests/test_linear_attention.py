@@ -585,3 +585,26 @@ def test_two_graphs_of_a_layer_in_turn(gpu, dtype):
             torch.cuda.synchronize()
             assert torch.equal(c.o, want[i][0]) and torch.equal(c.sT, want[i][1])
     del graphs
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Hkv,Dk,Dv,lengths", [
+    (520, 3, 2, 1, 64, 96, [520, 385, 257]),
+    (400, 2, 3, 3, 192, 40, [400, 130]),
+    (520, 4, 2, 2, 128, 136, [0, 128, 129, 513]),
+    (600, 1, 4, 4, 24, 200, None),
+])
+def test_a_few_pieces_with_and_without_state(gpu, T, B, H, Hkv, Dk, Dv, lengths, dtype):
+    c = Case(T, B, H, Hkv, Dk, Dv, dtype, lengths, decay=[1.0, 0.0, 0.5, 1.0 - 2.0 ** -12][:H])
+    assert 3 <= rnn.rnn_linear_attention_plan_query(H, Hkv, Dk, Dv, dtype, T, B)[1]["pieces"] <= 4
+    assert c.forward() == rnn.RNN_OK
+    c.check()
+    s0 = c.s0.clone()
+    c.sT = c.s0                            # in place
+    assert c.forward() == rnn.RNN_OK
+    c.s0 = s0
+    c.check()
+    c.s0, c.sT = None, s0.clone()
+    assert c.forward() == rnn.RNN_OK
+    c.check()
