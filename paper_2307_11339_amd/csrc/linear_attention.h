@@ -77,11 +77,11 @@ inline int la_waves(int Dk, int Dv) {
 // Numbers of one (piece, sequence, head, block of columns) in the seams.
 inline __host__ __device__ int64_t la_seam(int key_tiles, int waves) { return (int64_t)waves * 2 * key_tiles * 256; }
 
-// Waves of a SIMD that the tiles in LDS leave room for (workgroups of 58 to 66 KB stand two on a compute unit, smaller ones
+// Waves of a SIMD that the tiles in LDS leave room for (workgroups of 57 to 73 KB stand two on a compute unit, smaller ones
 // three or four), and so the registers that a wave may have.
 constexpr int la_waves_a_simd(int key_tiles, int waves, bool states) {
     if (key_tiles > 4 || waves == 2 || (key_tiles > 2 && waves == 4 && !states)) return 2;
-    return waves == 8 || key_tiles == 1 ? 4 : 3;
+    return waves == 8 || (key_tiles == 1 && states) ? 4 : 3;
 }
 
 // Where a workgroup of a chunk kernel works.  Workgroups go to the eight XCDs in turn: those that read the same keys

@@ -5,9 +5,8 @@
 //   S'  = decay^n S + sum_j k_j (decay^(n-1-j) v_j)^T
 // Each wave owns 16 columns of S and of o, S in its accumulators (fp32) from the first chunk to the last; only the scores
 // pass between waves, through LDS.  All products are 16 x 16 x 32 bf16 matrix instructions with fp32 sums.  What is
-// no bf16 number by itself is handed over as several of them, each the rounded rest of those before: scores times powers of
-// the decay, and the state as an operand, as two (16 bits, far below the rounding of the bf16 output); weighted values as three
-// (24 bits: the state is an fp32 result).
+// no bf16 number by itself (scores times powers of the decay, the state as an operand, weighted values) is handed over as three
+// of them, each the rounded rest of those before: 24 bits, as many as fp32 has.
 //
 // Operand layouts.  Of a 16 x 16 result, lane l holds column l % 16 and rows 4 (l / 16) + 0..3; as an operand of the next
 // product it has to hold eight neighbouring indices of a sum of 32, 8 (l / 16) + 0..7.  So a pair of results of the state
@@ -36,6 +35,7 @@ typedef __attribute__((address_space(3))) bf16x4 lds_bf16x4;
 
 constexpr int C = LA_CHUNK;
 constexpr int P_ROW = 2 * C;          // bytes of a row of scores
+constexpr int PARTS = 3;              // bf16 numbers that hold one of fp32
 
 __device__ inline f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
@@ -63,7 +63,6 @@ __device__ inline uint32_t round2(float& x, float& y) {
 }
 
 // x = the sum of PARTS bf16 numbers up to 2^(-8 PARTS) of it
-template <int PARTS>
 __device__ inline void split(const float* x, bf16x8 (&part)[PARTS]) {
     union { bf16x8 v; uint32_t u[4]; } out[PARTS];
 #pragma unroll
@@ -85,7 +84,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
     __shared__ __attribute__((aligned(1024))) char sq[STATES ? 16 : KeyTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sk[KeyTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sv[ValueTile::BYTES];
-    __shared__ __attribute__((aligned(1024))) char sp[STATES ? 16 : 2 * C * P_ROW];       // scores [i][j]: rounded, rest
+    __shared__ __attribute__((aligned(1024))) char sp[STATES ? 16 : PARTS * C * P_ROW];       // scores [part][i][j]
     __shared__ __attribute__((aligned(16))) float power[C + 4], before[16 + C + 4], weight[C];
 
     float* const scaled = before + 16;             // scale decay^i, and zeros for scores behind the diagonal
@@ -135,7 +134,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
     if (tid < 16) before[tid] = 0.f;
     if (!STATES) {
         // the blocks of scores behind the diagonal that take part in products of 32 steps: rows 0, columns 1 and 2, 3 of 16
-        for (int i = tid; i < 2 * 2 * 16 * 2; i += THREADS) {
+        for (int i = tid; i < PARTS * 2 * 16 * 2; i += THREADS) {
             const int piece = i & 1, row = i >> 1 & 15, block = i >> 5 & 1, part = i >> 6;
             *reinterpret_cast<la_u32x4*>(sp + part * C * P_ROW + la_piece<P_ROW>(32 * block + row, 4 * block + 2 + piece)) = la_u32x4{0, 0, 0, 0};
         }
@@ -245,14 +244,14 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                     for (int e = 0; e < 4; ++e) asm volatile("" : "+v"(p[e]));
 #pragma unroll
                     for (int e = 0; e < 4; ++e) p[e] = i >= j + e ? s[z][e] * p[e] : 0.f;
-                    uint2 hi, lo;
-                    hi.x = round2(p[0], p[1]);
-                    hi.y = round2(p[2], p[3]);
-                    lo.x = round2(p[0], p[1]);
-                    lo.y = round2(p[2], p[3]);
                     char* to = sp + la_piece<P_ROW>(i, 2 * J[z] + (g >> 1)) + 8 * (g & 1);
-                    *reinterpret_cast<uint2*>(to) = hi;
-                    *reinterpret_cast<uint2*>(to + C * P_ROW) = lo;
+#pragma unroll
+                    for (int part = 0; part < PARTS; ++part) {
+                        uint2 w;
+                        w.x = round2(p[0], p[1]);
+                        w.y = round2(p[2], p[3]);
+                        *reinterpret_cast<uint2*>(to + part * C * P_ROW) = w;
+                    }
                 }
             };
 #pragma unroll 1
@@ -267,12 +266,12 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                 for (int x = 0; x < KT; ++x) {
                     const float s8[8] = {S[2 * x][0], S[2 * x][1], S[2 * x][2], S[2 * x][3],
                                          S[2 * x + 1][0], S[2 * x + 1][1], S[2 * x + 1][2], S[2 * x + 1][3]};
-                    bf16x8 part[2], b[4];
+                    bf16x8 part[PARTS], b[4];
 #pragma unroll
                     for (int I = 0; I < 4; ++I) b[I] = read8(sq + I * 16 * KR + la_block(row_at, x));
-                    split<2>(s8, part);
+                    split(s8, part);
 #pragma unroll
-                    for (int p = 0; p < 2; ++p)
+                    for (int p = PARTS - 1; p >= 0; --p)
 #pragma unroll
                         for (int I = 0; I < 4; ++I) out[I] = mma(part[p], b[I], out[I]);
                 }
@@ -293,10 +292,10 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
             for (int s = 0; s < 2; ++s) {
                 const bf16x8 vv = read_transposed(v_a + 32 * s * VR, v_b + 32 * s * VR);
                 float wv[8];
-                bf16x8 part[3];
+                bf16x8 part[PARTS];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) wv[e] = (float)vv[e] * weight[32 * s + 8 * g + e];
-                split<3>(wv, part);
+                split(wv, part);
 #pragma unroll
                 for (int x = 0; x < KT; ++x) {
                     bf16x8 kk[2];
@@ -304,7 +303,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                     for (int p = 0; p < 2; ++p)
                         kk[p] = read_transposed(sk + 32 * s * KR + 8 * p + la_block(kt_a, x), sk + 32 * s * KR + 8 * p + la_block(kt_b, x));
 #pragma unroll
-                    for (int j = 0; j < 3; ++j)
+                    for (int j = 0; j < PARTS; ++j)
 #pragma unroll
                         for (int p = 0; p < 2; ++p) S[2 * x + p] = mma(kk[p], part[j], S[2 * x + p]);
                 }
@@ -326,7 +325,9 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                         for (int I = 0; I < 4; ++I) {
                             const int i = 16 * I + l16;
                             const char* px = sp + la_piece<P_ROW>(i, j >> 3) + 2 * (j & 7);
-                            const float p = bf16_to_f32(*(const bf16_t*)px) + bf16_to_f32(*(const bf16_t*)(px + C * P_ROW));
+                            float p = 0.f;
+#pragma unroll
+                            for (int part = 0; part < PARTS; ++part) p += bf16_to_f32(*(const bf16_t*)(px + part * C * P_ROW));
 #pragma unroll
                             for (int e = 0; e < 4; ++e) {
                                 const float x = bf16_to_f32(((const bf16_t*)vx)[e]);
@@ -342,7 +343,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
 #pragma unroll
                 for (int s = 0; s < 2; ++s)
 #pragma unroll
-                    for (int p = 0; p < 2; ++p)
+                    for (int p = 0; p < PARTS; ++p)
 #pragma unroll
                         for (int I = 2 * s; I < 4; ++I)
                             out[I] = mma(vv[s], read8(sp + p * C * P_ROW + I * 16 * P_ROW + (p_at ^ (s << 6))), out[I]);

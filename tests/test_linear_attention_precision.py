@@ -1,0 +1,73 @@
+"""How precise linear attention is inside, where the rounding of its outputs does not hide it.
+
+u = 2^-24, the rounding of fp32; an output's own rounding is 2^-8 (bf16) or u (fp32) of it.  Each bound counts the roundings
+that a result passes through; terms that cancel show what their roundings leave.
+"""
+import pytest
+
+from paper_2307_11339_amd import rnn
+from test_linear_attention import Case, gpu  # noqa: F401  (the fixture)
+
+F32, BF16 = rnn.RNN_F32, rnn.RNN_BF16
+U = 2.0 ** -24
+OWN = {F32: U, BF16: 2.0 ** -8}
+
+pytestmark = pytest.mark.gpu
+
+
+def _clear(c):
+    for x in (c.q, c.k, c.v, c.s0):
+        if x is not None:
+            x.zero_()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Dk,Dv", [(8, 2, 2, 16, 64), (64, 1, 3, 128, 128), (70, 2, 1, 40, 24), (1100, 1, 1, 64, 64), (20, 1, 2, 256, 256)])
+def test_states_that_cancel(gpu, T, B, H, Dk, Dv, dtype):
+    """q reads the sum of two rows of an initial state that differ in their last twelve bits.  The state is the same at every
+    step (decay 1, no keys).  The two terms of each output pass through eight additions and multiplications at most (three
+    parts of each, the scale, the chunk's factor): 8 u of their sum of magnitudes.  An operand of 16 bits would lose 2^-17."""
+    torch = gpu
+    c = Case(T, B, H, H, Dk, Dv, dtype, decay=[1.0] * H, scale=1.0)
+    _clear(c)
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = 1.0 + torch.rand((B, H, Dv), device="cuda", generator=gen)
+    c.s0[:, :, 1] = x
+    c.s0[:, :, Dk - 2] = -(x + torch.rand((B, H, Dv), device="cuda", generator=gen) * 2.0 ** -12)
+    c.q[..., 1] = 1
+    c.q[..., Dk - 2] = 1
+    assert c.forward() == rnn.RNN_OK
+    torch.cuda.synchronize()
+    want = c.s0.double().sum(2)
+    mass = c.s0.double().abs().sum(2)
+    off = (c.o.double() - want).abs() / (8 * U * mass + OWN[dtype] * want.abs())
+    assert float(off.max()) <= 1, float(off.max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Dk,Dv", [(32, 3, 4, 16, 16), (32, 2, 16, 128, 128), (30, 2, 5, 72, 40)])
+def test_scores_that_cancel(gpu, T, B, H, Dk, Dv, dtype):
+    """Two neighbouring steps have the same key and opposite values, so an output is the difference of two scores that lie a
+    part of 2^-12 apart: o_i = a b (decay^(i-1) - decay^i), for step 0's value -1 and step 1's 1.  A score passes through the
+    rounding of a power, of the scale in it, of the product and of its parts, an output through two sums: 8 u of the two scores'
+    magnitudes.  Scores of 16 bits would lose 2^-17."""
+    torch = gpu
+    lam = 1.0 - 2.0 ** -12
+    c = Case(T, B, H, H, Dk, Dv, dtype, decay=[lam] * H, scale=0.75, state=False)
+    _clear(c)
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    a = (1.0 + torch.rand((T, B, H), device="cuda", generator=gen)).to(c.tdt)
+    b = (1.0 + torch.rand((B, H), device="cuda", generator=gen)).to(c.tdt)
+    c.q[..., Dk // 2] = a
+    c.k[0, ..., Dk // 2] = b
+    c.k[1, ..., Dk // 2] = b
+    c.v[0] = -1
+    c.v[1] = 1
+    assert c.forward() == rnn.RNN_OK
+    torch.cuda.synchronize()
+    t = torch.arange(T, device="cuda", dtype=torch.float64).view(T, 1, 1)
+    ab = 0.75 * a.double() * b.double()
+    far, near = lam ** t * ab, torch.where(t >= 1, lam ** (t - 1), torch.zeros_like(t)) * ab
+    want = (near - far)[..., None]
+    off = (c.o.double() - want).abs() / (8 * U * (near + far)[..., None] + OWN[dtype] * want.abs())
+    assert float(off.max()) <= 1, float(off.max())
