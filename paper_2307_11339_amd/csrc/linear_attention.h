@@ -194,21 +194,17 @@ struct LaTile {
     static constexpr int PER_ROW = WIDTH / VEC, AT_ONCE = THREADS / PER_ROW, N = (ROWS + AT_ONCE - 1) / AT_ONCE;
     static constexpr int BYTES = ROWS * ROW;
     la_u32x4 reg[N];
-    uint32_t offset;                 // of the first piece
-    // stride: bytes between rows, at least those of `width` elements and at most 2^25: 64 rows end before 2^31, and what is to
-    // be zero is read from there on
-    __device__ inline void init(uint32_t stride, int width) {
-        const int row = threadIdx.x / PER_ROW, piece = threadIdx.x % PER_ROW;
-        offset = row < AT_ONCE && piece * VEC < width ? (uint32_t)row * stride + piece * 16 : 0x80000000u;
-    }
-    // n >= 1 rows from `from` on, the same for all threads
-    __device__ inline void load(const T* from, uint32_t stride, int width, int n) {
+    // n >= 1 rows from `from` on, the same for all threads.  stride: bytes between rows, at least those of `width` elements and at
+    // most 2^25: 64 rows end before 2^31, and what is to be zero is read from there on.  thread: its number, fresh (the place is
+    // found anew instead of being kept).
+    __device__ inline void load(const T* from, uint32_t stride, int width, int n, int thread) {
+        const int row = thread / PER_ROW, piece = thread % PER_ROW;
         const __amdgpu_buffer_rsrc_t rows = la_rows(from, stride, width, min(n, ROWS));
-        const uint32_t first = la_fresh(offset);
+        const uint32_t first = row < AT_ONCE && piece * VEC < width ? (uint32_t)row * stride + piece * 16 : 0x80000000u;
 #pragma unroll
         for (int i = 0; i < N; ++i) reg[i] = __builtin_amdgcn_raw_buffer_load_b128(rows, first + i * AT_ONCE * stride, 0, 0);
     }
-    // thread: its number, fresh (the place is found anew instead of being kept)
+    // thread: likewise
     __device__ inline void store(char* lds, int thread) const {
         const int row = thread / PER_ROW, piece = thread % PER_ROW;
         if (THREADS % PER_ROW == 0 || row < AT_ONCE) {

@@ -40,6 +40,16 @@ constexpr int PARTS = 3;              // bf16 numbers that hold one of fp32
 __device__ inline f32x4 mma(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 
 __device__ inline bool finite(float x) { return fabsf(x) < __builtin_inff(); }
+// All eight: the largest exponent of the eight, two numbers at a time.
+__device__ inline bool finite(bf16x8 x) {
+    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+    union { bf16x8 v; u16x2 h[4]; } w;
+    w.v = x;
+    u16x2 most = w.h[0] & (uint16_t)0x7fff;
+#pragma unroll
+    for (int i = 1; i < 4; ++i) most = __builtin_elementwise_max(most, (u16x2)(w.h[i] & (uint16_t)0x7fff));
+    return max(most[0], most[1]) < 0x7f80;
+}
 
 __device__ inline bf16x8 read8(const char* p) { return *reinterpret_cast<const bf16x8*>(p); }
 
@@ -105,14 +115,11 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
 
     KeyTile tq, tk;
     ValueTile tv;
-    if (!STATES) tq.init((uint32_t)a.qs.t * 2, a.Dk);
-    tk.init((uint32_t)a.ks.t * 2, a.Dk);
-    tv.init((uint32_t)a.vs.t * 2, cols);
     auto load = [&](int c) {
-        const int n = live - c * C;
-        if (!STATES) tq.load(q + (int64_t)c * C * a.qs.t, (uint32_t)a.qs.t * 2, a.Dk, n);
-        tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 2, a.Dk, n);
-        tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 2, cols, n);
+        const int n = live - c * C, thread = la_fresh(tid);
+        if (!STATES) tq.load(q + (int64_t)c * C * a.qs.t, (uint32_t)a.qs.t * 2, a.Dk, n, thread);
+        tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 2, a.Dk, n, thread);
+        tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 2, cols, n, thread);
     };
     // gain: of the state before chunk c
     auto store = [&](int c, float gain) {
@@ -200,6 +207,12 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
     if (chunks) store(0, 1.f);
     __syncthreads();
 
+    // The wave's columns of 32 values, transposed: rows 8 g + l16 / 4 and four further, four columns at l16 % 4.
+    auto values = [&](int s, int l16, int g) {
+        const int row = 8 * g + (l16 >> 2), piece = 2 * wave + (l16 >> 1 & 1), half = 8 * (l16 & 1);
+        return read_transposed(sv + la_piece<VR>(row, piece) + half + 32 * s * VR, sv + la_piece<VR>(row + 4, piece) + half + 32 * s * VR);
+    };
+
     float gain = 1.f;             // what S is to be multiplied by
 #pragma unroll 1
     for (int c = 0; c < chunks; ++c) {
@@ -209,11 +222,6 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         // the lane's places in the tiles; found anew for each chunk: they are cheap, and registers are short
         const int l16 = la_fresh(lane & 15), g = la_fresh(lane >> 4);
         const int row_at = la_piece<KR>(l16, g), p_at = la_piece<P_ROW>(l16, g);
-        // transposed: rows 8 g + l16 / 4 and four further, four columns at l16 % 4 (of the state's order, of the wave's own)
-        const int tr = 8 * g + (l16 >> 2), tc = l16 & 3;
-        const int kt_a = la_piece<KR>(tr, tc), kt_b = la_piece<KR>(tr + 4, tc);
-        const char* v_a = sv + la_piece<VR>(tr, 2 * wave + (tc >> 1)) + 8 * (tc & 1);
-        const char* v_b = sv + la_piece<VR>(tr + 4, 2 * wave + (tc >> 1)) + 8 * (tc & 1);
         if (!STATES) {
             // scores: blocks of 16 rows j and 16 columns i on and below the diagonal, ten in all; two at a time where a wave
             // has two, so that one's reads and products fill the other's waits
@@ -284,39 +292,11 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         gain *= power[n];
         const bool small = gain < LA_LEAST_GAIN;
         if (mine) {
-            if (small) {
-#pragma unroll
-                for (int y = 0; y < 2 * KT; ++y) S[y] *= gain;
-            }
-#pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const bf16x8 vv = read_transposed(v_a + 32 * s * VR, v_b + 32 * s * VR);
-                float wv[8];
-                bf16x8 part[PARTS];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) wv[e] = (float)vv[e] * weight[32 * s + 8 * g + e];
-                split(wv, part);
-#pragma unroll
-                for (int x = 0; x < KT; ++x) {
-                    bf16x8 kk[2];
-#pragma unroll
-                    for (int p = 0; p < 2; ++p)
-                        kk[p] = read_transposed(sk + 32 * s * KR + 8 * p + la_block(kt_a, x), sk + 32 * s * KR + 8 * p + la_block(kt_b, x));
-#pragma unroll
-                    for (int j = 0; j < PARTS; ++j)
-#pragma unroll
-                        for (int p = 0; p < 2; ++p) S[2 * x + p] = mma(kk[p], part[j], S[2 * x + p]);
-                }
-                __builtin_amdgcn_sched_barrier(0);      // operands of one half at a time: there are no registers for both
-            }
             if (!STATES) {
-                // A value that is not finite, times the zero above the diagonal, would reach steps before its own.  It makes
-                // every row of its column of the state not finite: where one is, such values are left out of the product and
-                // added to the steps that they belong to.
-                bf16x8 vv[2];
-#pragma unroll
-                for (int s = 0; s < 2; ++s) vv[s] = read_transposed(v_a + 32 * s * VR, v_b + 32 * s * VR);
-                const bool strange = __builtin_amdgcn_ballot_w64(!finite(S[0][0])) != 0;
+                // A value that is not finite, times the zero above the diagonal, would reach steps before its own: such values are
+                // left out of the product and added to the steps that they belong to.
+                bf16x8 vv[2] = {values(0, l16, g), values(1, l16, g)};
+                const bool strange = __builtin_amdgcn_ballot_w64(!(finite(vv[0]) && finite(vv[1]))) != 0;
                 if (strange) {
 #pragma unroll 1
                     for (int j = 0; j < C; ++j) {
@@ -357,6 +337,38 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                     w[1] = round2(r[2], r[3]);
                     __builtin_amdgcn_raw_buffer_store_b64(w, rows, at_o + 16 * I * (uint32_t)a.os.t * 2, 0, 0);
                 }
+            }
+            // What the chunk adds is summed up by itself: the state, which may be far larger, is then rounded once a chunk.
+            const int row = 8 * g + (l16 >> 2), k_a = la_piece<KR>(row, l16 & 3), k_b = la_piece<KR>(row + 4, l16 & 3);
+            if (small) {
+#pragma unroll
+                for (int y = 0; y < 2 * KT; ++y) S[y] *= gain;
+            }
+            bf16x8 part[2][PARTS];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const bf16x8 vv = values(s, l16, g);
+                float wv[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) wv[e] = (float)vv[e] * weight[32 * s + 8 * g + e];
+                split(wv, part[s]);
+            }
+#pragma unroll
+            for (int x = 0; x < KT; ++x) {
+                f32x4 add[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    bf16x8 kk[2];
+#pragma unroll
+                    for (int p = 0; p < 2; ++p)
+                        kk[p] = read_transposed(sk + 32 * s * KR + 8 * p + la_block(k_a, x), sk + 32 * s * KR + 8 * p + la_block(k_b, x));
+#pragma unroll
+                    for (int j = PARTS - 1; j >= 0; --j)
+#pragma unroll
+                        for (int p = 0; p < 2; ++p) add[p] = mma(kk[p], part[s][j], add[p]);
+                }
+#pragma unroll
+                for (int p = 0; p < 2; ++p) S[2 * x + p] += add[p];
             }
         }
         if (small) gain = 1.f;

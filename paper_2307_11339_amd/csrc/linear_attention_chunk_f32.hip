@@ -55,14 +55,11 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
 
     KeyTile tq, tk;
     ValueTile tv;
-    if (!STATES) tq.init((uint32_t)a.qs.t * 4, a.Dk);
-    tk.init((uint32_t)a.ks.t * 4, a.Dk);
-    tv.init((uint32_t)a.vs.t * 4, cols);
     auto load = [&](int c) {
-        const int n = live - c * C;
-        if (!STATES) tq.load(q + (int64_t)c * C * a.qs.t, (uint32_t)a.qs.t * 4, a.Dk, n);
-        tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 4, a.Dk, n);
-        tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 4, cols, n);
+        const int n = live - c * C, thread = la_fresh(tid);
+        if (!STATES) tq.load(q + (int64_t)c * C * a.qs.t, (uint32_t)a.qs.t * 4, a.Dk, n, thread);
+        tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 4, a.Dk, n, thread);
+        tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 4, cols, n, thread);
     };
     // gain: of the state before chunk c
     auto store = [&](int c, float gain) {
@@ -205,37 +202,19 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         gain *= power[n];
         const bool small = gain < LA_LEAST_GAIN;
         if (mine) {
-            if (small) {
-#pragma unroll
-                for (int y = 0; y < 2 * KT; ++y) S[y] *= gain;
-            }
-#pragma unroll
-            for (int s = 0; s < BLOCKS; ++s) {
-                f32x4 wv;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) wv[e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
-                wv *= *reinterpret_cast<const f32x4*>(weight + 16 * s + 4 * g);
-#pragma unroll
-                for (int y = 0; y < 2 * KT; y += 2) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-#pragma unroll
-                        for (int z = 0; z < 2; ++z)
-                            S[y + z] = mma(*reinterpret_cast<const float*>(sk + 16 * s * KR + la_block(k_at[e], y + z)), wv[e], S[y + z]);
-                    if (KT >= 4 && y % 4 == 2) __builtin_amdgcn_sched_barrier(0);
-                }
-                __builtin_amdgcn_sched_barrier(0);      // operands of one half at a time: there are no registers for both
-            }
             if (!STATES) {
-                // A value that is not finite, times the zero above the diagonal, would reach steps before its own.  It makes
-                // every row of its column of the state not finite: where one is, such values are left out of the product and
-                // added to the steps that they belong to.
+                // A value that is not finite, times the zero above the diagonal, would reach steps before its own: such values are
+                // left out of the product and added to the steps that they belong to.
                 f32x4 vv[BLOCKS];
+                float zero = 0.f;              // or NaN
 #pragma unroll
                 for (int s = 0; s < BLOCKS; ++s)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) vv[s][e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
-                const bool strange = __builtin_amdgcn_ballot_w64(!finite(S[0][0])) != 0;
+                    for (int e = 0; e < 4; ++e) {
+                        vv[s][e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
+                        zero = fmaf(vv[s][e], 0.f, zero);
+                    }
+                const bool strange = __builtin_amdgcn_ballot_w64(!finite(zero)) != 0;
                 if (strange) {
 #pragma unroll 1
                     for (int j = 0; j < C; ++j) {
@@ -272,6 +251,35 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                     for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(out[I][e]);
                     __builtin_amdgcn_raw_buffer_store_b128(w, rows, at_o + 16 * I * (uint32_t)a.os.t * 4, 0, 0);
                 }
+            }
+            __builtin_amdgcn_sched_barrier(0);      // the outputs are out of the way: there are no registers for both
+            // What the chunk adds is summed up by itself: the state, which may be far larger, is then rounded once a chunk.
+            if (small) {
+#pragma unroll
+                for (int y = 0; y < 2 * KT; ++y) S[y] *= gain;
+            }
+            f32x4 wv[BLOCKS];
+#pragma unroll
+            for (int s = 0; s < BLOCKS; ++s) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) wv[s][e] = *reinterpret_cast<const float*>(sv + 16 * s * VR + v_at[e]);
+                wv[s] *= *reinterpret_cast<const f32x4*>(weight + 16 * s + 4 * g);
+            }
+#pragma unroll
+            for (int y = 0; y < 2 * KT; y += 2) {
+                f32x4 add[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+                for (int s = 0; s < BLOCKS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+#pragma unroll
+                        for (int z = 0; z < 2; ++z)
+                            add[z] = mma(*reinterpret_cast<const float*>(sk + 16 * s * KR + la_block(k_at[e], y + z)), wv[s][e], add[z]);
+#pragma unroll
+                for (int z = 0; z < 2; ++z) S[y + z] += add[z];
+                // one by one: operands of several would not fit
+                asm volatile("" : "+v"(S[y]), "+v"(S[y + 1]));
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (small) gain = 1.f;

@@ -71,3 +71,23 @@ def test_scores_that_cancel(gpu, T, B, H, Dk, Dv, dtype):
     want = (near - far)[..., None]
     off = (c.o.double() - want).abs() / (8 * U * (near + far)[..., None] + OWN[dtype] * want.abs())
     assert float(off.max()) <= 1, float(off.max())
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Dk,Dv", [(2048, 64, 17, 8, 16), (2048, 16, 10, 128, 128)])
+def test_a_long_sum_is_rounded_once_a_chunk(gpu, T, B, H, Dk, Dv, dtype):
+    """Decay 1: the state of step T is the sum of T products.  One fp32 rounding is off by 0.42 u (root mean square, of values
+    spread over a binade).  Sums of C steps (32 in fp32, 64 in bf16) that are added to the state one by one leave it
+    0.42 u sqrt(T / C / 2) off, as the state grows like the square root of the steps; inside a sum, of at most C roundings,
+    0.42 u sqrt(C / 2).  Of the 2-norms of both a quarter more is allowed.  Products added to the state itself, four at a time
+    in fp32, would leave 0.42 u sqrt(T / 8)."""
+    torch = gpu
+    c = Case(T, B, H, H, Dk, Dv, dtype, decay=[1.0] * H, state=False)
+    chunk = 32 if dtype == F32 else 64
+    plan = rnn.rnn_linear_attention_plan_query(H, H, Dk, Dv, dtype, T, B)[1]
+    assert plan["pieces"] == 1 and plan["chunk"] == chunk
+    assert c.forward() == rnn.RNN_OK
+    k, v = (x.double().permute(1, 2, 0, 3) for x in (c.k, c.v))
+    want = torch.matmul(k.transpose(-1, -2).contiguous(), v.contiguous())
+    off = float((c.sT.double() - want).norm() / want.norm())
+    assert off <= 1.25 * 0.42 * U * (T / chunk / 2 + chunk / 2) ** 0.5, off / U
