@@ -175,6 +175,9 @@ __device__ inline int la_fresh(int x) {
     return x;
 }
 
+// A number that is the same in all lanes, out of the vector registers.
+__device__ inline float la_uniform(float x) { return __uint_as_float(__builtin_amdgcn_readfirstlane(__float_as_uint(x))); }
+
 constexpr int la_row_bytes(int bytes) { return bytes <= 64 ? 64 : bytes <= 128 ? 128 : bytes <= 256 ? 256 : bytes <= 512 ? 512 : 1024; }
 
 typedef __attribute__((ext_vector_type(4))) uint32_t la_u32x4;

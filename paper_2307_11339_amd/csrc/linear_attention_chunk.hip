@@ -121,16 +121,12 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 2, a.Dk, n, thread);
         tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 2, cols, n, thread);
     };
-    // gain: of the state before chunk c
-    auto store = [&](int c, float gain) {
+    auto store = [&](int c) {
         const int n = min(C, live - c * C), thread = la_fresh(tid);
         if (!STATES) tq.store(sq, thread);
         tk.store(sk, thread);
         tv.store(sv, thread);
-        if (tid < C) {
-            const float next = gain * power[n];
-            weight[tid] = tid < n ? power[n - 1 - tid] * (next < LA_LEAST_GAIN ? 1.f : 1.f / next) : 0.f;
-        }
+        if (tid < C) weight[tid] = tid < n ? power[n - 1 - tid] : 0.f;
     };
     const int chunks = (live + C - 1) / C;
     // loads come back in order: this one first, then the first tiles and the state, nothing waited for between them
@@ -204,7 +200,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         scaled[tid] = my_power * a.scale;
     }
     __syncthreads();
-    if (chunks) store(0, 1.f);
+    if (chunks) store(0);
     __syncthreads();
 
     // The wave's columns of 32 values, transposed: rows 8 g + l16 / 4 and four further, four columns at l16 % 4.
@@ -289,8 +285,9 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
             __syncthreads();       // the scores are there
             if (c + 1 < chunks) load(c + 1);        // not before: the operands above need the registers
         }
-        gain *= power[n];
+        gain = la_uniform(gain * power[n]);
         const bool small = gain < LA_LEAST_GAIN;
+        const float rise = la_uniform(small ? 1.f : 1.f / gain);      // of what the chunk adds, where the state has not fallen
         if (mine) {
             if (!STATES) {
                 // A value that is not finite, times the zero above the diagonal, would reach steps before its own: such values are
@@ -368,12 +365,14 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                         for (int p = 0; p < 2; ++p) add[p] = mma(kk[p], part[s][j], add[p]);
                 }
 #pragma unroll
-                for (int p = 0; p < 2; ++p) S[2 * x + p] += add[p];
+                for (int p = 0; p < 2; ++p)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S[2 * x + p][e] = fmaf(rise, add[p][e], S[2 * x + p][e]);
             }
         }
         if (small) gain = 1.f;
         __syncthreads();           // the tiles are used up
-        if (c + 1 < chunks) store(c + 1, gain);
+        if (c + 1 < chunks) store(c + 1);
         __syncthreads();
     }
 

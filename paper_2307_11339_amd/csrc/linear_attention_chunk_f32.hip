@@ -61,16 +61,12 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         tk.load(k + (int64_t)c * C * a.ks.t, (uint32_t)a.ks.t * 4, a.Dk, n, thread);
         tv.load(v + (int64_t)c * C * a.vs.t, (uint32_t)a.vs.t * 4, cols, n, thread);
     };
-    // gain: of the state before chunk c
-    auto store = [&](int c, float gain) {
+    auto store = [&](int c) {
         const int n = min(C, live - c * C), thread = la_fresh(tid);
         if (!STATES) tq.store(sq, thread);
         tk.store(sk, thread);
         tv.store(sv, thread);
-        if (tid < C) {
-            const float next = gain * power[n];
-            weight[step_place(tid)] = tid < n ? power[n - 1 - tid] * (next < LA_LEAST_GAIN ? 1.f : 1.f / next) : 0.f;
-        }
+        if (tid < C) weight[step_place(tid)] = tid < n ? power[n - 1 - tid] : 0.f;
     };
     const int chunks = (live + C - 1) / C;
     // loads come back in order: this one first, then the first tiles and the state, nothing waited for between them
@@ -136,7 +132,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         scaled[tid] = my_power * a.scale;
     }
     __syncthreads();
-    if (chunks) store(0, 1.f);
+    if (chunks) store(0);
     __syncthreads();
 
     float gain = 1.f;             // what S is to be multiplied by
@@ -199,8 +195,9 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
             __syncthreads();       // the scores are there
             if (c + 1 < chunks) load(c + 1);        // not before: the operands above need the registers
         }
-        gain *= power[n];
+        gain = la_uniform(gain * power[n]);
         const bool small = gain < LA_LEAST_GAIN;
+        const float rise = la_uniform(small ? 1.f : 1.f / gain);      // of what the chunk adds, where the state has not fallen
         if (mine) {
             if (!STATES) {
                 // A value that is not finite, times the zero above the diagonal, would reach steps before its own: such values are
@@ -276,7 +273,9 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                         for (int z = 0; z < 2; ++z)
                             add[z] = mma(*reinterpret_cast<const float*>(sk + 16 * s * KR + la_block(k_at[e], y + z)), wv[s][e], add[z]);
 #pragma unroll
-                for (int z = 0; z < 2; ++z) S[y + z] += add[z];
+                for (int z = 0; z < 2; ++z)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) S[y + z][e] = fmaf(rise, add[z][e], S[y + z][e]);
                 // one by one: operands of several would not fit
                 asm volatile("" : "+v"(S[y]), "+v"(S[y + 1]));
                 __builtin_amdgcn_sched_barrier(0);
@@ -284,7 +283,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         }
         if (small) gain = 1.f;
         __syncthreads();           // the tiles are used up
-        if (c + 1 < chunks) store(c + 1, gain);
+        if (c + 1 < chunks) store(c + 1);
         __syncthreads();
     }
 

@@ -91,3 +91,16 @@ def test_a_long_sum_is_rounded_once_a_chunk(gpu, T, B, H, Dk, Dv, dtype):
     want = torch.matmul(k.transpose(-1, -2).contiguous(), v.contiguous())
     off = float((c.sT.double() - want).norm() / want.norm())
     assert off <= 1.25 * 0.42 * U * (T / chunk / 2 + chunk / 2) ** 0.5, off / U
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,B,lengths", [(20, 2, None), (200, 3, [200, 64, 129]), (1300, 1, None)])
+def test_large_values_of_small_keys(gpu, T, B, lengths, dtype):
+    """Values of some 2^120, keys of 2^-60: everything in the formula stays far inside fp32's range, whatever the decay."""
+    c = Case(T, B, 4, 2, 64, 48, dtype, lengths, decay=[0.9, 0.97, 0.5, 1.0])
+    c.v.mul_(2.0 ** 120)
+    c.k.mul_(2.0 ** -60)
+    c.s0.mul_(2.0 ** 60)
+    assert bool(c.v.isfinite().all())
+    assert c.forward() == rnn.RNN_OK
+    c.check()
