@@ -36,6 +36,8 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
     __shared__ __attribute__((aligned(1024))) char sv[ValueTile::BYTES];
     __shared__ __attribute__((aligned(1024))) char sp[STATES ? 16 : C * P_ROW];           // scores [i][j]
     __shared__ __attribute__((aligned(16))) float power[C + 4], before[16 + C + 4], weight[C];
+    __shared__ double fall[2];                     // decay^C; the power that the state held is to be multiplied by
+    __shared__ float behind;                       // the latter, behind the chunk in the tiles
 
     float* const scaled = before + 16;             // scale decay^i, and zeros for scores behind the diagonal
     LaPlace at;
@@ -66,15 +68,31 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         if (!STATES) tq.store(sq, thread);
         tk.store(sk, thread);
         tv.store(sv, thread);
-        if (tid < C) weight[step_place(tid)] = tid < n ? power[n - 1 - tid] : 0.f;
+        if (thread < C) {                             // at most a wave
+            weight[step_place(thread)] = thread < n ? power[n - 1 - thread] : 0.f;
+            // in 64 bits: the same rounding in every chunk would add up
+            const double next = fall[1] * (n == C ? fall[0] : power[n]);
+            if (thread == 0) {
+                behind = (float)next;
+                fall[1] = (float)next < LA_LEAST_GAIN ? 1.0 : next;
+            }
+        }
     };
     const int chunks = (live + C - 1) / C;
+    static_assert(C <= 64, "fall is read by the wave that writes it");
     // loads come back in order: this one first, then the first tiles and the state, nothing waited for between them
     static_assert(THREADS > C, "a thread for each power");
     const float my_power = a.powers[at.h * (LA_CHUNK + 1) + min(tid, C)];
     if (chunks) load(0);
 
     if (tid < 16) before[tid] = 0.f;
+    if (tid == 1) {                                // which has the decay itself
+        double whole = my_power;
+#pragma unroll
+        for (int n = 1; n < C; n *= 2) whole *= whole;
+        fall[0] = whole;
+        fall[1] = 1.0;
+    }
     // state: element e of result y = row 16 y + 4 g + e, column l % 16 of the wave's
     const int my_col = 16 * wave + l16;
     const int64_t state_at = ((int64_t)at.b * a.H + at.h) * a.Dk * a.Dv + at.v0;
@@ -142,7 +160,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
         if (STATES && c + 1 < chunks) load(c + 1);
         f32x4 out[BLOCKS];
         // the lane's places in the tiles; found anew for each chunk: they are cheap, and registers are short
-        const int l16 = la_fresh(lane & 15), g = la_fresh(lane >> 4);
+        const int thread = la_fresh(tid), l16 = thread & 15, g = thread >> 4 & 3;
         const int row_at = la_piece<KR>(l16, g), p_at = la_piece<P_ROW>(l16, g);
         // steps 4 e + g: rows of keys (16 columns of block y) and values (the wave's own)
         int k_at[4], v_at[4];
@@ -195,7 +213,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
             __syncthreads();       // the scores are there
             if (c + 1 < chunks) load(c + 1);        // not before: the operands above need the registers
         }
-        gain = la_uniform(gain * power[n]);
+        gain = la_uniform(behind);
         const bool small = gain < LA_LEAST_GAIN;
         const float rise = la_uniform(small ? 1.f : 1.f / gain);      // of what the chunk adds, where the state has not fallen
         if (mine) {

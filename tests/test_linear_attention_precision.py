@@ -104,3 +104,36 @@ def test_large_values_of_small_keys(gpu, T, B, lengths, dtype):
     assert bool(c.v.isfinite().all())
     assert c.forward() == rnn.RNN_OK
     c.check()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,B,H,Dk,Dv", [(2048, 57, 9, 8, 64), (4096, 2, 9, 32, 32)])
+def test_a_state_decays_by_the_power_of_its_steps(gpu, T, B, H, Dk, Dv, dtype):
+    """No keys: a state is decay^T of what it was, an output the sum of one row of it.  Decays for which the roundings of
+    decay^32 and decay^64 are far from their means, so that a product of rounded powers would run off by a fraction of u for
+    each chunk.  A number passes through a rounded power (u), the product with it (u) and, every time that the state has
+    fallen by 2^10, two more of these (the power itself may be off by one unit in its last place, 2 u); for the pieces of a
+    sequence, at most 32 here, another 4 u each that is joined; a row of one element is exact as an operand."""
+    torch = gpu
+    decay = [0.99997, 0.9999, 0.9995, 0.999, 0.997, 0.99, 1.0 - 2.0 ** -13, 0.99993, 0.99985]
+    lam = torch.tensor(decay, dtype=torch.float32, device="cuda").double()
+    c = Case(T, B, H, H, Dk, Dv, dtype, decay=decay, scale=1.0)
+    c.k.zero_()
+    c.v.zero_()
+    c.q.zero_()
+    c.q[..., 3] = 1
+    plan = rnn.rnn_linear_attention_plan_query(H, H, Dk, Dv, dtype, T, B)[1]
+    assert plan["chunk"] and (plan["pieces"] == 1) == (B == 57)
+    assert c.forward() == rnn.RNN_OK
+    torch.cuda.synchronize()
+    left = lam ** T
+    folds = (-torch.log2(left) / 10).floor() + 1
+    allowed = (3 + 4 * folds + (4 * plan["pieces"] if plan["pieces"] > 1 else 0)) * U
+    s0 = c.s0.double()
+    want = s0 * left.view(1, H, 1, 1)
+    off = ((c.sT.double() - want).abs() / want.abs()).amax((0, 2, 3)) / allowed
+    assert float(off.max()) <= 1, off
+    t = torch.arange(1, T + 1, device="cuda", dtype=torch.float64).view(T, 1, 1, 1)
+    want = lam.view(1, 1, H, 1) ** t * s0[None, :, :, 3]
+    off = ((c.o.double() - want).abs() / want.abs()).amax((0, 1, 3)) / (allowed + OWN[dtype])
+    assert float(off.max()) <= 1, off
