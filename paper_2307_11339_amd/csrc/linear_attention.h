@@ -141,13 +141,18 @@ inline int64_t la_grid(LaArgs* args, int pieces) {
     return (units + 7) / 8 * 8 * a.rep * a.vblocks;
 }
 
-// decay^n from its logarithm, which is 0 or less: to fp32's rounding whatever n
-__device__ inline float la_power(double log2_decay, int n) {
-    const double y = n * log2_decay;
-    if (!(y > -160.0)) return 0.f;
-    const double whole = floor(y);
-    return ldexpf(exp2f((float)(y - whole)), (int)whole);
-}
+// decay^n from its logarithm, which is 0 or less, as two numbers: rounded, the state of many pieces in a row would run off by
+// the same rounding for each.
+struct LaPower {
+    float high, low;
+    __device__ inline LaPower(double log2_decay, int n) {
+        const double power = exp2(n * log2_decay);
+        high = (float)power;
+        low = (float)(power - high);
+    }
+    // a state that long later, and what was added
+    __device__ inline float on(float state, float add) const { return fmaf(high, state, fmaf(low, state, add)); }
+};
 
 // Tiles in LDS: rows of ROW bytes (64 to 1024), whose pieces of 16 bytes change places from row to row, so that the ways of
 // reading a tile find their pieces in different banks: one piece of each of 16 rows (an operand whose index of the sum

@@ -174,7 +174,7 @@ __global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a, int64_t pe
     if (i >= all) return;
     const uint32_t block = (uint32_t)(i / per), unit = block / a.vblocks, b = unit / a.H, h = unit - b * a.H;
     const int len = min(a.lengths ? a.lengths[b] : a.T, a.T);
-    const float decay = la_power(a.log2_decay[h], a.piece_steps);
+    const LaPower decay(a.log2_decay[h], a.piece_steps);
     int live = 1;                                      // pieces that have steps to start
     while (live < a.pieces && len > live * a.piece_steps) ++live;
     if (live <= 2) return;
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a, int64_t pe
         for (int j = 0; j < AT_ONCE; ++j) {
             if (p0 + j >= live) break;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) run[e] = fmaf(decay, run[e], add[j][e]);
+            for (int e = 0; e < 4; ++e) run[e] = decay.on(run[e], add[j][e]);
             *reinterpret_cast<f32x4*>(a.seams + (p0 + j) * all + i) = run;
         }
     }

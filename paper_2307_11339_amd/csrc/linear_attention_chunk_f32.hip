@@ -108,7 +108,7 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
 #pragma unroll
         for (int y = 0; y < 2 * KT; ++y) S[y] = from[y * 64];
         if (!a.joined && at.piece > 1) {               // what the pieces before this one add
-            const float decay = la_power(a.log2_decay[at.h], a.piece_steps);
+            const LaPower decay(a.log2_decay[at.h], a.piece_steps);
             constexpr int AT_ONCE = KT <= 4 ? 2 : 1;   // as registers allow: loads under way together
 #pragma unroll 1
             for (int p = 2; p <= at.piece; p += AT_ONCE) {
@@ -121,7 +121,9 @@ __global__ __launch_bounds__(64 * NW, la_waves_a_simd(KT, NW, STATES)) void la_c
                 for (int j = 0; j < AT_ONCE; ++j)
                     if (p + j <= at.piece) {
 #pragma unroll
-                        for (int y = 0; y < 2 * KT; ++y) S[y] = decay * S[y] + add[j][y];
+                        for (int y = 0; y < 2 * KT; ++y)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) S[y][e] = decay.on(S[y][e], add[j][y][e]);
                     }
             }
         }

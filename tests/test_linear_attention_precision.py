@@ -137,3 +137,31 @@ def test_a_state_decays_by_the_power_of_its_steps(gpu, T, B, H, Dk, Dv, dtype):
     want = lam.view(1, 1, H, 1) ** t * s0[None, :, :, 3]
     off = ((c.o.double() - want).abs() / want.abs()).amax((0, 1, 3)) / (allowed + OWN[dtype])
     assert float(off.max()) <= 1, off
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+def test_many_pieces_decay_by_the_power_of_their_steps(gpu, dtype):
+    """As above, over hundreds of pieces that are joined.  A number is rounded once for each piece that it is carried over, off
+    by 0.42 u (root mean square) each, in one direction or the other: of n of them 0.42 u sqrt(n).  A rounded power would
+    be off in the same direction every time.  Of the 2-norm a quarter more is allowed, and 8 u for the piece itself and its ends."""
+    torch = gpu
+    T, decay = 131072, [0.99999, 0.999995]
+    lam = torch.tensor(decay, dtype=torch.float32, device="cuda").double()
+    c = Case(T, 1, 2, 2, 32, 32, dtype, decay=decay, scale=1.0)
+    c.k.zero_()
+    c.v.zero_()
+    c.q.zero_()
+    c.q[..., 3] = 1
+    pieces = rnn.rnn_linear_attention_plan_query(2, 2, 32, 32, dtype, T, 1)[1]["pieces"]
+    assert pieces >= 256
+    assert c.forward() == rnn.RNN_OK
+    torch.cuda.synchronize()
+    allowed = (1.25 * 0.42 * pieces ** 0.5 + 8) * U
+    for h in range(2):
+        want = c.s0[:, h].double() * lam[h] ** T
+        off = float((c.sT[:, h].double() - want).norm() / want.norm())
+        assert off <= allowed, (h, off / U, allowed / U)
+        t = torch.arange(1, T + 1, device="cuda", dtype=torch.float64).view(T, 1)
+        want = lam[h] ** t * c.s0[:, h, 3].double()
+        off = float((c.o[:, 0, h].double() - want).norm() / want.norm())
+        assert off <= allowed + OWN[dtype], (h, off / U)
