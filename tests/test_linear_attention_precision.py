@@ -3,6 +3,7 @@
 u = 2^-24, the rounding of fp32; an output's own rounding is 2^-8 (bf16) or u (fp32) of it.  Each bound counts the roundings
 that a result passes through; terms that cancel show what their roundings leave.
 """
+import numpy as np
 import pytest
 
 from paper_2307_11339_amd import rnn
@@ -12,8 +13,6 @@ F32, BF16 = rnn.RNN_F32, rnn.RNN_BF16
 U = 2.0 ** -24
 OWN = {F32: U, BF16: 2.0 ** -8}
 
-pytestmark = pytest.mark.gpu
-
 
 def _clear(c):
     for x in (c.q, c.k, c.v, c.s0):
@@ -21,6 +20,7 @@ def _clear(c):
             x.zero_()
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("T,B,H,Dk,Dv", [(8, 2, 2, 16, 64), (64, 1, 3, 128, 128), (70, 2, 1, 40, 24), (1100, 1, 1, 64, 64), (20, 1, 2, 256, 256)])
 def test_states_that_cancel(gpu, T, B, H, Dk, Dv, dtype):
@@ -44,6 +44,7 @@ def test_states_that_cancel(gpu, T, B, H, Dk, Dv, dtype):
     assert float(off.max()) <= 1, float(off.max())
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("T,B,H,Dk,Dv", [(32, 3, 4, 16, 16), (32, 2, 16, 128, 128), (30, 2, 5, 72, 40)])
 def test_scores_that_cancel(gpu, T, B, H, Dk, Dv, dtype):
@@ -73,6 +74,7 @@ def test_scores_that_cancel(gpu, T, B, H, Dk, Dv, dtype):
     assert float(off.max()) <= 1, float(off.max())
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("T,B,H,Dk,Dv", [(2048, 64, 17, 8, 16), (2048, 16, 10, 128, 128)])
 def test_a_long_sum_is_rounded_once_a_chunk(gpu, T, B, H, Dk, Dv, dtype):
@@ -93,6 +95,7 @@ def test_a_long_sum_is_rounded_once_a_chunk(gpu, T, B, H, Dk, Dv, dtype):
     assert off <= 1.25 * 0.42 * U * (T / chunk / 2 + chunk / 2) ** 0.5, off / U
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("T,B,lengths", [(20, 2, None), (200, 3, [200, 64, 129]), (1300, 1, None)])
 def test_large_values_of_small_keys(gpu, T, B, lengths, dtype):
@@ -106,6 +109,7 @@ def test_large_values_of_small_keys(gpu, T, B, lengths, dtype):
     c.check()
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("T,B,H,Dk,Dv", [(2048, 57, 9, 8, 64), (4096, 2, 9, 32, 32)])
 def test_a_state_decays_by_the_power_of_its_steps(gpu, T, B, H, Dk, Dv, dtype):
@@ -139,6 +143,7 @@ def test_a_state_decays_by_the_power_of_its_steps(gpu, T, B, H, Dk, Dv, dtype):
     assert float(off.max()) <= 1, off
 
 
+@pytest.mark.gpu
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 def test_many_pieces_decay_by_the_power_of_their_steps(gpu, dtype):
     """As above, over hundreds of pieces that are joined.  A number is rounded once for each piece that it is carried over, off
@@ -165,3 +170,56 @@ def test_many_pieces_decay_by_the_power_of_their_steps(gpu, dtype):
         want = lam[h] ** t * c.s0[:, h, 3].double()
         off = float((c.o[:, 0, h].double() - want).norm() / want.norm())
         assert off <= allowed + OWN[dtype], (h, off / U)
+
+
+ROW_OFF = 8 * U     # of a state's row that one step gave: a rounded power, the product, its parts and their sum, the factor of the
+                    # chunk's sum, the sum, the power that the state is held without, the product with it
+
+
+def _bf16(x):
+    """fp32 numbers rounded to bf16 (nearest, even)."""
+    bits = x.astype(np.float32).view(np.uint32).astype(np.uint64)
+    return ((bits + 0x7fff + (bits >> 16 & 1)) & 0xffff0000).astype(np.uint32).view(np.float32)
+
+
+def _row_case(T, seed=6):
+    """Values and the weights that they have in the state behind the last step."""
+    rng = np.random.default_rng(seed)
+    v = _bf16(rng.standard_normal((T, 40)))
+    lam = float(np.float32(0.987))
+    return v, lam, lam ** (T - 1 - np.arange(T))[:, None]
+
+
+def test_the_bound_on_a_row_notices_two_parts():
+    """Weighted values handed over as two bf16 numbers would pass a bound of 2^-16; three are far inside the one below."""
+    v, _, weight = _row_case(64)
+    x = v * weight.astype(np.float32)
+    off = []
+    for parts in (2, 3):
+        rest, got = x.copy(), np.zeros_like(x, dtype=np.float64)
+        for _ in range(parts):
+            part = _bf16(rest)
+            got += part
+            rest = rest - part
+        off.append((abs(got - v.astype(np.float64) * weight) / abs(v * weight)).max())
+    assert off[0] > 4 * ROW_OFF and off[1] < ROW_OFF / 2, off
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("T,Dk", [(20, 24), (64, 64), (100, 104), (250, 256)])
+def test_each_row_of_a_state_by_itself(gpu, T, Dk, dtype):
+    """Step j has the key e_j, so row j of the state is decay^(T-1-j) v_j, of one step alone."""
+    torch = gpu
+    v, lam, weight = _row_case(T)
+    c = Case(T, 1, 1, 1, Dk, 40, dtype, decay=[lam], state=False)
+    c.k.zero_()
+    for j in range(T):
+        c.k[j, 0, 0, j] = 1
+    c.v.copy_(torch.from_numpy(v)[:, None, None])
+    assert c.forward() == rnn.RNN_OK
+    torch.cuda.synchronize()
+    got = c.sT[0, 0].double().cpu().numpy()
+    want = v.astype(np.float64) * weight
+    assert (abs(got[:T] - want) <= ROW_OFF * abs(want)).all(), (abs(got[:T] - want) / abs(want)).max() / U
+    assert not got[T:].any()
