@@ -461,7 +461,8 @@ enum rnn_gate { RNN_GATE_NONE = 0, RNN_GATE_LINEAR = 1, RNN_GATE_SIGMOID = 2, RN
  * scale mean ones, NULL biases zeros; a vector of an absent norm is ignored.  eps > 0 and finite, groups a divisor of
  * width (else RNN_EINVAL).  Supported: width up to 16384, width and width / groups multiples of 4 (RNN_F32) or 8
  * (RNN_BF16), and width / groups at least 32 where after is not RNN_NORM_NONE and groups > 1; otherwise RNN_EUNSUPPORTED.
- * The call synchronises the device. */
+ * The call synchronises the device, before it reads vectors in device memory as well: work enqueued on any stream may still
+ * be writing them. */
 int rnn_block_norm_create(rnn_block_norm** out, int width, int dtype, int after, int groups, const void* after_weight,
                           const void* after_bias, int gate, const void* scale, int before, const void* before_weight,
                           const void* before_bias, float eps, int weights_on_device);

@@ -511,6 +511,12 @@ int rnn_block_norm_create(rnn_block_norm** out, int width, int dtype, int after,
             delete n;
             return RNN_ENOMEM;
         }
+        // The copies go through the null stream, which does not wait for what other streams have yet to write.
+        if (weights_on_device && hipDeviceSynchronize() != hipSuccess) {
+            (void)hipGetLastError();
+            rnn_block_norm_destroy(n);
+            return RNN_EDEVICE;
+        }
         size_t at = 0;
         for (int i = 0; i < 5; ++i) {
             if (!from[i]) continue;
