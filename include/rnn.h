@@ -92,7 +92,8 @@ enum rnn_plan { RNN_PLAN_AUTO = 0, RNN_PLAN_CELLWISE = 1, RNN_PLAN_WAVEFRONT = 2
  *                      (bf16 = the upper 16 bits of an IEEE float).  A NULL bias means zeros.
  *   weights_on_device  0: the pointed-to arrays are host memory; 1: device memory.
  * The library copies and repacks the weights; the caller keeps ownership of its arrays and may
- * free them when the call returns.  The call synchronises the device.
+ * free them when the call returns.  The call synchronises the device, before it reads weights in device memory as well: work
+ * enqueued on any stream may still be writing them (of rnn_model_set_peepholes the same is true).
  * Supported shapes: hidden_size a multiple of 4 for RNN_F32 and a multiple of 8 for RNN_BF16,
  * input_size a multiple of 8 for RNN_BF16; otherwise RNN_EUNSUPPORTED.
  * The persistent kernels exist for certain hidden sizes (bf16: 128 x {1, 2, 3, 4, 5, 6, 8, 10, 12, 16};

@@ -1282,8 +1282,9 @@ int rnn_model_create_ordered(rnn_model** out, int cell, int num_layers, int inpu
     m->esize = (dtype == RNN_BF16) ? 2 : 4;
     int rc = RNN_OK;
     hipDeviceProp_t prop;
-    if (hipGetDevice(&m->device) != hipSuccess ||
-        hipGetDeviceProperties(&prop, m->device) != hipSuccess) {
+    // the weights are read through the null stream, which does not wait for what other streams have yet to write
+    if (hipGetDevice(&m->device) != hipSuccess || hipGetDeviceProperties(&prop, m->device) != hipSuccess ||
+        (weights_on_device && hipDeviceSynchronize() != hipSuccess)) {
         (void)hipGetLastError();
         delete m;
         return RNN_EDEVICE;
@@ -1442,6 +1443,7 @@ int rnn_model_set_peepholes(rnn_model* m, const float* const* peepholes, int on_
     }
     if (m->cell != CELL_LSTM) return RNN_EUNSUPPORTED;
     const size_t bytes = (size_t)3 * m->H * sizeof(float);
+    if (on_device) HIP_TRY(hipDeviceSynchronize());      // the null stream does not wait for what other streams have yet to write
     std::vector<DevBuf> fresh((size_t)m->L * m->D);
     int rc = RNN_OK;
     for (size_t g = 0; g < fresh.size() && rc == RNN_OK; ++g) {
