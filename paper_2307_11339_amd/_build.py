@@ -45,6 +45,8 @@ NO_SPILL.update({"wavefront_xcd%s.hip" % part: ("wavefront_xcd_kernel", "") for 
 # The chunks of linear attention hold a state in registers and load the chunk to come while they work on one: a register that is
 # spilled on its way makes that load a wait.
 NO_SPILL.update({"linear_attention_chunk.hip": ("la_chunk_kernel", ""), "linear_attention_chunk_f32.hip": ("la_chunk_f32_kernel", "")})
+# The norms around a block read a row once, into registers: spilled, every row would go through memory again.
+NO_SPILL["block_norm.hip"] = ("block_norm_kernel", "")
 
 
 def _check_no_spill(src: str, remarks: str) -> None:

@@ -2,8 +2,9 @@
 //
 //   a = N_after(x) by groups;  a *= act(gate);  r = residual + scale a;  y = N_before(r)
 //
-// One pass: a row is read once into registers, every mean is taken from there (the variance from the differences to the
-// mean, so nothing cancels), and what is asked for is written once.  Bound by the bytes of its tensors.
+// One pass: a row is read once into registers (gate and residual of a wide one when they are needed), every mean is taken from
+// there (the variance from the differences to the mean, so nothing cancels), and what is asked for is written once.  Bound by
+// the bytes of its tensors.
 //
 // Layout.  A row is a line of slots, one piece of 16 bytes each (or three of one group); thread i of the row's `waves`
 // waves holds slots i, i + 64 waves, .. (VPT pieces in all).  A group starts a power of two of slots, or a whole number of 64, so that 64 neighbouring
@@ -117,7 +118,7 @@ struct Sums {
     float (*buf)[NORM_CHUNKS];
     int turn;
     // of all: `lanes` threads in a wave, or all threads of `waves` waves
-    __device__ inline float row(float v, int lanes, int waves) {
+    __device__ __forceinline__ float row(float v, int lanes, int waves) {
         v = sum_in_wave(v, lanes);
         if (waves == 1) return v;
         float* b = buf[turn];
@@ -129,7 +130,7 @@ struct Sums {
         return s;
     }
     // of each group; v[i]: what the thread has of slot i's group, replaced by that group's sum
-    __device__ inline void groups(float (&v)[VPT], int lanes, int waves, int deep) {
+    __device__ __forceinline__ void groups(float (&v)[VPT], int lanes, int waves, int deep) {
         if (deep > 1) {                                // slots of whole groups; pieces behind a multiple of deep are none
 #pragma unroll
             for (int i = 1; i < VPT; ++i) v[i] += i % deep ? v[i - 1] : 0.f;
@@ -145,7 +146,7 @@ struct Sums {
         const int chunks = lanes >> 6;                 // 64 slots each that a group takes
         if (chunks <= 1) return;
         float s[VPT];
-        if (waves == 1) {
+        if (VPT <= 2 && waves == 1) {                  // a wave holds two pieces a thread at most (norm_divide)
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
                 s[i] = 0.f;
@@ -173,20 +174,25 @@ struct Sums {
     }
 };
 
+// A piece of a row, `at` bytes behind its beginning: 32 bits, so that the beginning stays in scalar registers and no address
+// of 64 bits has to be kept for each piece and tensor.
+__device__ inline uint4 read_piece(const void* row, uint32_t at) { return *reinterpret_cast<const uint4*>((const char*)row + at); }
+__device__ inline void write_piece(void* row, uint32_t at, const uint4& v) { *reinterpret_cast<uint4*>((char*)row + at) = v; }
+
 template <typename T, int VPT>
-__device__ inline void normalise(float (&f)[VPT][Piece<T>::N], const float* factor, const T* w, const T* c, const int* col, const bool* has) {
+__device__ inline void normalise(float (&f)[VPT][Piece<T>::N], const float* factor, const T* w, const T* c, const uint32_t* at, const bool* has) {
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
         float x[Piece<T>::N];
 #pragma unroll
         for (int e = 0; e < Piece<T>::N; ++e) f[i][e] *= factor[i];
         if (w && has[i]) {
-            Piece<T>::unpack(*reinterpret_cast<const uint4*>(w + col[i]), x);
+            Piece<T>::unpack(read_piece(w, at[i]), x);
 #pragma unroll
             for (int e = 0; e < Piece<T>::N; ++e) f[i][e] *= x[e];
         }
         if (c && has[i]) {
-            Piece<T>::unpack(*reinterpret_cast<const uint4*>(c + col[i]), x);
+            Piece<T>::unpack(read_piece(c, at[i]), x);
 #pragma unroll
             for (int e = 0; e < Piece<T>::N; ++e) f[i][e] += x[e];
         }
@@ -197,6 +203,9 @@ __device__ inline void normalise(float (&f)[VPT][Piece<T>::N], const float* fact
 template <typename T, int VPT, bool AFTER, bool GATE, bool BEFORE, bool WAVE_ROW>
 __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormArgs a) {
     constexpr int N = Piece<T>::N;
+    // Of wide rows the gate and the residual are asked for when they are needed: there are no registers to hold all three.  (8192
+    // rows of 128 gated fp32 heads of 128, everything at once: 590 us, 905 with all three held and spilled.)
+    constexpr bool WIDE = VPT >= 8;
     __shared__ float buf[2][NORM_CHUNKS];
     Sums<VPT> sums;
     sums.buf = buf;
@@ -207,7 +216,7 @@ __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormA
     const int gw = a.W / a.groups;                      // width of a group
     const uint4 zero = make_uint4(0, 0, 0, 0);
 
-    int col[VPT];
+    uint32_t at[VPT];                                   // of a piece in its row, in bytes
     bool has[VPT];
 #pragma unroll
     for (int i = 0; i < VPT; ++i) {
@@ -215,7 +224,7 @@ __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormA
         const unsigned slot = WAVE_ROW ? (pass * waves + (waves == 1 ? 0 : wave)) * 64 + lane : threadIdx.x % (unsigned)a.lay.slots;
         const unsigned group = slot / (unsigned)a.lay.lanes, c = (slot % (unsigned)a.lay.lanes + in_group * a.lay.lanes) * N;
         has[i] = (int)c < gw && (int)group < a.groups;
-        col[i] = has[i] ? group * gw + c : 0;
+        at[i] = has[i] ? (group * gw + c) * (uint32_t)sizeof(T) : 0;
     }
 
     const uint32_t rows = (uint32_t)a.T * a.B, step = gridDim.x * a.lay.rows;        // at most 2^30 and 2^21
@@ -235,20 +244,24 @@ __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormA
         for (int i = 0; i < VPT; ++i) {
             px[i] = pg[i] = pr[i] = zero;
             if (!live || !has[i]) continue;
-            px[i] = *reinterpret_cast<const uint4*>(x + col[i]);
-            if (GATE) pg[i] = *reinterpret_cast<const uint4*>(gate + col[i]);
-            if (a.residual) pr[i] = *reinterpret_cast<const uint4*>(residual + col[i]);
+            px[i] = read_piece(x, at[i]);
+            if (GATE && !WIDE) pg[i] = read_piece(gate, at[i]);
+            if (a.residual && !WIDE) pr[i] = read_piece(residual, at[i]);
         }
     };
     for (uint32_t r0 = blockIdx.x * a.lay.rows; r0 < rows; r0 += step) {
+        if (WIDE) {                                        // new numbers for the compiler: or it keeps an address for each piece and vector
+#pragma unroll
+            for (int i = 0; i < VPT; ++i) asm volatile("" : "+v"(at[i]));
+        }
         load(r0 + sub);
         if (WAVE_ROW && !live) {                           // a wave's rows, and with barriers a workgroup's, are one
             if (in) {
 #pragma unroll
                 for (int i = 0; i < VPT; ++i) {
                     if (!has[i]) continue;
-                    if (a.residual_out) *reinterpret_cast<uint4*>((T*)a.residual_out + t * a.os.t + b * a.os.b + col[i]) = zero;
-                    if (a.y) *reinterpret_cast<uint4*>((T*)a.y + t * a.ys.t + b * a.ys.b + col[i]) = zero;
+                    if (a.residual_out) write_piece((T*)a.residual_out + t * a.os.t + b * a.os.b, at[i], zero);
+                    if (a.y) write_piece((T*)a.y + t * a.ys.t + b * a.ys.b, at[i], zero);
                 }
             }
             continue;
@@ -259,7 +272,7 @@ __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormA
 
         if (AFTER) {
             float s[VPT];
-            auto sum = [&]() {
+            auto sum = [&]() __attribute__((always_inline)) {
                 if (a.groups > 1) return sums.groups(s, a.lay.lanes, waves, a.lay.deep);
                 float all = 0.f;
 #pragma unroll
@@ -290,11 +303,13 @@ __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormA
             sum();
 #pragma unroll
             for (int i = 0; i < VPT; ++i) s[i] = 1.0f / sqrtf(s[i] * a.per_group + a.eps);
-            normalise<T, VPT>(f, s, (const T*)a.aw, (const T*)a.ab, col, has);
+            normalise<T, VPT>(f, s, (const T*)a.aw, (const T*)a.ab, at, has);
         }
         if (GATE) {
+            const T* gate = (const T*)a.gate + t * a.gs.t + b * a.gs.b;
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
+                if (WIDE && has[i]) pg[i] = read_piece(gate, at[i]);
                 float z[N];
                 Piece<T>::unpack(pg[i], z);
                 if (a.act == RNN_GATE_SILU) {
@@ -314,14 +329,16 @@ __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormA
             for (int i = 0; i < VPT; ++i)
                 if (has[i]) {
                     float w[N];
-                    Piece<T>::unpack(*reinterpret_cast<const uint4*>((const T*)a.sc + col[i]), w);
+                    Piece<T>::unpack(read_piece(a.sc, at[i]), w);
 #pragma unroll
                     for (int e = 0; e < N; ++e) f[i][e] *= w[e];
                 }
         }
         if (a.residual) {
+            const T* residual = (const T*)a.residual + t * a.rs.t + b * a.rs.b;
 #pragma unroll
             for (int i = 0; i < VPT; ++i) {
+                if (WIDE && has[i]) pr[i] = read_piece(residual, at[i]);
                 float c[N];
                 Piece<T>::unpack(pr[i], c);
 #pragma unroll
@@ -332,7 +349,7 @@ __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormA
             T* to = (T*)a.residual_out + t * a.os.t + b * a.os.b;
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
-                if (has[i]) *reinterpret_cast<uint4*>(to + col[i]) = live ? Piece<T>::pack(f[i]) : zero;
+                if (has[i]) write_piece(to, at[i], live ? Piece<T>::pack(f[i]) : zero);
         }
         if (!a.y) continue;                                // the same for all threads
         if (BEFORE) {
@@ -357,13 +374,13 @@ __global__ __launch_bounds__(64 * NORM_WAVES) void block_norm_kernel(const NormA
             s = 1.0f / sqrtf(sums.row(s, row_lanes, waves) * a.per_row + a.eps);
 #pragma unroll
             for (int i = 0; i < VPT; ++i) factor[i] = s;
-            normalise<T, VPT>(f, factor, (const T*)a.bw, (const T*)a.bb, col, has);
+            normalise<T, VPT>(f, factor, (const T*)a.bw, (const T*)a.bb, at, has);
         }
         if (in) {
             T* to = (T*)a.y + t * a.ys.t + b * a.ys.b;
 #pragma unroll
             for (int i = 0; i < VPT; ++i)
-                if (has[i]) *reinterpret_cast<uint4*>(to + col[i]) = live ? Piece<T>::pack(f[i]) : zero;
+                if (has[i]) write_piece(to, at[i], live ? Piece<T>::pack(f[i]) : zero);
         }
     }
 }
@@ -420,9 +437,26 @@ void launch_norm_vpt(const NormArgs& a, unsigned grid, unsigned threads, hipStre
     }
 }
 
+// More than eight pieces a thread: groups in fp32 whose slots are hardly more than half full.  (bf16 rows have half as many pieces,
+// rows that are one group no empty slots: false, and nothing is launched.)
+template <typename T> bool launch_norm_widest(const NormArgs&, unsigned, unsigned, hipStream_t) { return false; }
+template <> bool launch_norm_widest<float>(const NormArgs& a, unsigned grid, unsigned threads, hipStream_t stream) {
+    if (!a.after || a.lay.vpt > 16) return false;
+    switch ((a.act ? 2 : 0) + (a.before ? 1 : 0)) {
+    case 0: block_norm_kernel<float, 16, true, false, false, true><<<grid, threads, 0, stream>>>(a); break;
+    case 1: block_norm_kernel<float, 16, true, false, true, true><<<grid, threads, 0, stream>>>(a); break;
+    case 2: block_norm_kernel<float, 16, true, true, false, true><<<grid, threads, 0, stream>>>(a); break;
+    default: block_norm_kernel<float, 16, true, true, true, true><<<grid, threads, 0, stream>>>(a); break;
+    }
+    return true;
+}
+
 template <typename T>
-void launch_norm(const NormArgs& a, unsigned grid, unsigned threads, hipStream_t stream) {
-    if (a.lay.rows > 4) return launch_norm_vpt<T, 1, false>(a, grid, threads, stream);
+bool launch_norm(const NormArgs& a, unsigned grid, unsigned threads, hipStream_t stream) {
+    if (a.lay.rows > 4) {
+        launch_norm_vpt<T, 1, false>(a, grid, threads, stream);
+        return true;
+    }
     switch (a.lay.vpt) {
     case 1: launch_norm_vpt<T, 1, true>(a, grid, threads, stream); break;
     case 2: launch_norm_vpt<T, 2, true>(a, grid, threads, stream); break;
@@ -432,8 +466,9 @@ void launch_norm(const NormArgs& a, unsigned grid, unsigned threads, hipStream_t
     case 6: launch_norm_vpt<T, 6, true>(a, grid, threads, stream); break;
     case 7:
     case 8: launch_norm_vpt<T, 8, true>(a, grid, threads, stream); break;
-    default: launch_norm_vpt<T, 16, true>(a, grid, threads, stream); break;
+    default: return launch_norm_widest<T>(a, grid, threads, stream);
     }
+    return true;
 }
 
 bool row_view(const int64_t* strides, int T, int B, int width, int step, bool output, RowView* out) {
@@ -583,8 +618,9 @@ int rnn_block_norm_forward(const rnn_block_norm* n, const void* x, const int64_t
     // 199 us, 213 with as many as it holds and 195 with one row a wave; but 65536 rows of 16 gated heads 158, 167 and 172.
     const int64_t most = (int64_t)n->cus * 8192 / threads;
     const unsigned grid = (unsigned)(wgs < most ? wgs : most);
-    if (n->dtype == RNN_BF16) launch_norm<bf16_t>(a, grid, threads, (hipStream_t)stream);
-    else launch_norm<float>(a, grid, threads, (hipStream_t)stream);
+    const bool known = n->dtype == RNN_BF16 ? launch_norm<bf16_t>(a, grid, threads, (hipStream_t)stream)
+                                            : launch_norm<float>(a, grid, threads, (hipStream_t)stream);
+    if (!known) return RNN_EUNSUPPORTED;
     return hipGetLastError() == hipSuccess ? RNN_OK : RNN_EDEVICE;
 }
 

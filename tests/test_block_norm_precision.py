@@ -241,3 +241,21 @@ def test_rows_that_are_hard_to_norm_one_by_one(gpu, W, dtype, row):
         c.x[..., W // 2] = 3.0
     assert c.forward() == rnn.RNN_OK
     _hold(torch, c)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,W,groups", [(F32, 16384, 1), (F32, 15860, 61), (F32, 7540, 29), (BF16, 15080, 29), (BF16, 16384, 1)])
+def test_wide_rows_over_their_own_inputs(gpu, dtype, W, groups):
+    """Inputs that are read late are still read before anything is written over them."""
+    torch = gpu
+    c = Case(5, 3, W, dtype, after=LAYER, groups=groups, gate=G_SILU, before=RMS, lengths=[5, 0, 3])
+    assert c.forward() == rnn.RNN_OK
+    _hold(torch, c)
+    inputs = {n: getattr(c, n).clone() for n in ("x", "gate", "residual")}
+    y, out = c.y.clone(), c.out.clone()
+    for to_y, to_out in (("x", "residual"), ("gate", "x"), ("residual", "gate"), ("gate", "residual")):
+        for n, t in inputs.items():
+            getattr(c, n).copy_(t)
+        assert c.forward(y=getattr(c, to_y), out=getattr(c, to_out)) == rnn.RNN_OK
+        torch.cuda.synchronize()
+        assert torch.equal(getattr(c, to_y), y) and torch.equal(getattr(c, to_out), out)
