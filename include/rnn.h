@@ -395,7 +395,8 @@ int rnn_linear_attention_create(rnn_linear_attention** out, int num_heads, int n
 void rnn_linear_attention_destroy(rnn_linear_attention* layer);
 
 /* Allocate the layer's workspace now if forwards of T steps and B sequences use one (long sequences of few heads do:
- * the states at the seams of the pieces they are split into).  One size serves every shape, so nothing ever grows. */
+ * the states at the seams of the pieces they are split into).  One size serves every shape, so nothing ever grows: 8 MiB for
+ * each 32 of key_size up to 128, 48 MiB up to 192 and 64 MiB beyond.  RNN_EUNSUPPORTED if T * B > 2^30. */
 int rnn_linear_attention_reserve(rnn_linear_attention* layer, int T, int B);
 
 /*

@@ -257,8 +257,10 @@ int check_shape(int H, int Hkv, int Dk, int Dv, int dtype) {
     return RNN_OK;
 }
 
-int check_call(int H, int T, int B, const LaPlan& p) {
-    if ((int64_t)T * B > ((int64_t)1 << 30)) return RNN_EUNSUPPORTED;
+// Before choose(), whose sums of steps stay below 2^31 for what passes here.
+int check_steps(int T, int B) { return (int64_t)T * B > ((int64_t)1 << 30) ? RNN_EUNSUPPORTED : RNN_OK; }
+
+int check_call(int H, int B, const LaPlan& p) {
     // workgroups of one launch, of 512 threads at most: with what la_grid adds, fewer than 2^32 threads
     return (int64_t)B * H * p.pieces * p.vblocks > (1 << 22) ? RNN_EUNSUPPORTED : RNN_OK;
 }
@@ -379,9 +381,10 @@ int rnn_linear_attention_plan_query(int num_heads, int num_kv_heads, int key_siz
                                     int B, int* plan) {
     if (!plan || T < 1 || B < 1) return RNN_EINVAL;
     int rc = check_shape(num_heads, num_kv_heads, key_size, value_size, dtype);
+    if (rc == RNN_OK) rc = check_steps(T, B);
     if (rc != RNN_OK) return rc;
     const LaPlan p = choose(num_heads, key_size, value_size, dtype, T, B);
-    rc = check_call(num_heads, T, B, p);
+    rc = check_call(num_heads, B, p);
     if (rc != RNN_OK) return rc;
     plan[0] = p.chunk; plan[1] = p.vblocks; plan[2] = p.pieces; plan[3] = p.piece_steps;
     return RNN_OK;
@@ -389,6 +392,8 @@ int rnn_linear_attention_plan_query(int num_heads, int num_kv_heads, int key_siz
 
 int rnn_linear_attention_reserve(rnn_linear_attention* l, int T, int B) {
     if (!l || T < 1 || B < 1) return RNN_EINVAL;
+    const int rc = check_steps(T, B);
+    if (rc != RNN_OK) return rc;
     if (l->seams || choose(l->H, l->Dk, l->Dv, l->dtype, T, B).pieces == 1) return RNN_OK;
     int device = -1;
     if (hipGetDevice(&device) != hipSuccess) {
@@ -413,8 +418,10 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
     if (!l || !q || !k || !v || !o || T < 1 || B < 1) return RNN_EINVAL;
     if (((uintptr_t)q | (uintptr_t)k | (uintptr_t)v | (uintptr_t)o | (uintptr_t)s0 | (uintptr_t)sT) & 15) return RNN_EINVAL;
     if ((uintptr_t)lengths & 3) return RNN_EINVAL;
+    int rc = check_steps(T, B);
+    if (rc != RNN_OK) return rc;
     LaPlan p = choose(l->H, l->Dk, l->Dv, l->dtype, T, B);
-    int rc = check_call(l->H, T, B, p);
+    rc = check_call(l->H, B, p);
     if (rc != RNN_OK) return rc;
     const int step = l->dtype == RNN_BF16 ? 8 : 4;
     LaArgs a = {};
@@ -425,7 +432,7 @@ int rnn_linear_attention_forward(rnn_linear_attention* l, const void* q, const i
     if (p.chunk && !(chunk_rows(a.qs, T, l->Dk, l->dtype) && chunk_rows(a.ks, T, l->Dk, l->dtype) && chunk_rows(a.vs, T, l->Dv, l->dtype) &&
                      chunk_rows(a.os, T, l->Dv, l->dtype))) {
         p = steps_plan(l->Dv, T);
-        rc = check_call(l->H, T, B, p);
+        rc = check_call(l->H, B, p);
         if (rc != RNN_OK) return rc;
     }
     int device = -1;
