@@ -415,7 +415,8 @@ int rnn_linear_attention_reserve(rnn_linear_attention* layer, int T, int B);
  * DEVICE pointers, 16-byte aligned.  o must not overlap an input.  The call enqueues work on `stream` and returns.
  * It allocates device memory only the first time that a shape uses the workspace (see rnn_linear_attention_reserve).
  * Non-finite inputs reach the outputs that depend on them by the formula, and no others (an infinity may come out as NaN).
- * States are held up to 2^10 times as large while the call runs: finite ones beyond 2^117 may overflow.
+ * States are held up to 2^10 times as large while the call runs: finite ones beyond 2^117 may overflow.  Runs of steps go by the
+ * sum over j above, so the products q_t . k_j and their terms have to stay within fp32 as well.
  * Stream capture: may be recorded into a HIP graph; RNN_EUNSUPPORTED, with nothing recorded, if the workspace would have to be
  * allocated first.  One forward in flight per layer (a replay counts), as the workspace is the layer's.
  * RNN_EINVAL if the layer belongs to another device than the current one.  RNN_EUNSUPPORTED if T * B > 2^30 or
@@ -449,7 +450,8 @@ int rnn_linear_attention_plan_query(int num_heads, int num_kv_heads, int key_siz
  *   r = residual + scale * a                       (r = scale * a without a residual)
  *   y = N_before(r) * before_weight + before_bias  the whole row; the input of the next block (y = r without this norm)
  * Every part but x may be absent.  All of it is computed in fp32 from the inputs; r and y are rounded once, when stored
- * (N_before sees r before it is rounded).
+ * (N_before sees r before it is rounded).  A row of finite values whose squares add up beyond fp32 (values of some 2^60) has 0 as
+ * the factor of its norm.
  */
 typedef struct rnn_block_norm rnn_block_norm;
 

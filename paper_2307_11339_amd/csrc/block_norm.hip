@@ -85,7 +85,7 @@ template <> struct Piece<bf16_t> {
         for (int i = 0; i < 8; ++i) o.h[i] = (__bf16)f[i];      // to nearest, even
         return o.u;
     }
-    // one unit in the last place of fp32, far below a bf16 rounding
+    // off by the rounding of the exponent's argument, some 2 |z| + 3 units of fp32: far below a bf16 rounding
     static __device__ inline float sigmoid(float z) { return __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
     static __device__ inline float silu(float z) { return z * __builtin_amdgcn_rcpf(1.0f + __expf(-z)); }
 };
@@ -392,7 +392,7 @@ int pow2_at_least(int n) {
 }
 
 // The slots of a row.  Groups of some widths would leave many slots empty, of ten pieces six; three pieces to a slot leave two
-// of twelve (33000 rows of 26 groups of 80 bf16 values: 127 us against 156).
+// of twelve (33000 gated rows of 26 groups of 80 bf16 values: 100 us against 117).
 bool norm_slots(int width, int groups, int vec, NormLayout* out) {
     const int pieces = width / groups / vec, third = (pieces + 2) / 3;
     out->deep = groups > 1 && pieces <= 64 && 5 * pow2_at_least(pieces) >= 6 * 3 * pow2_at_least(third) ? 3 : 1;
@@ -405,9 +405,9 @@ bool norm_slots(int width, int groups, int vec, NormLayout* out) {
 // How `rows` rows are divided.  Rows that are few are spread over as many waves as they have pieces for, until there is
 // a wave for every SIMD of the GPU (64 rows of 1024 bf16 values: 3.7 us with one piece a thread, 4.3 with two, 5.1 with four).
 // Many rows take as few waves each as hold two pieces a thread: more pieces leave too few waves a SIMD, fewer cost barriers.
-// 65536 rows of 2048 bf16 values, sum and norm: 201 us with two, 206 with four (and no barrier) or one; 17157 padded rows of 1280 fp32
-// values, everything at once: 92 with two or three, 103 with one, 110 with five; 16384 rows of 16 gated fp32 heads of 128: 80 with
-// two, 90 with three; 65536 of bf16 ones 158 with two, 176 with four.  (32768 rows of 8192: 400 with two, 392 with four.)
+// 65536 rows of 2048 bf16 values, sum and norm: 195 us with two, 199 with four (and no barrier), 198 with one; 17157 padded rows of 1280
+// fp32 values, everything at once: 80 with two, 86 with four, 99 with one; 16384 rows of 16 gated fp32 heads of 128: 77 with two, 100
+// with four, 80 with one; 65536 of bf16 ones 144 with two, 170 with four, 150 with one.  (32768 rows of 8192: 396, 392 with up to four.)
 void norm_divide(NormLayout* l, int64_t rows, int simds) {
     if (l->slots <= 32 && (l->slots & (l->slots - 1)) == 0 && l->deep == 1) {
         l->waves = l->vpt = 1;
@@ -615,7 +615,7 @@ int rnn_block_norm_forward(const rnn_block_norm* n, const void* x, const int64_t
     const int64_t wgs = (rows + a.lay.rows - 1) / a.lay.rows;
     const unsigned threads = a.lay.rows > 4 ? 256 : 64 * a.lay.waves * a.lay.rows;
     // Four times what the GPU holds at once: workgroups of a few rows each take what has become free.  131072 rows of 1024 bf16 values
-    // 199 us, 213 with as many as it holds and 195 with one row a wave; but 65536 rows of 16 gated heads 158, 167 and 172.
+    // 193 us, 212 with as many as it holds and 192 with one row a wave; but 65536 rows of 16 gated heads 144, 158 and 153.
     const int64_t most = (int64_t)n->cus * 8192 / threads;
     const unsigned grid = (unsigned)(wgs < most ? wgs : most);
     const bool known = n->dtype == RNN_BF16 ? launch_norm<bf16_t>(a, grid, threads, (hipStream_t)stream)

@@ -60,7 +60,8 @@ hipError_t la_launch_chunks_f32(const LaArgs& a, int key_tiles, int waves, bool 
 // Blocks of 32 rows that a chunk kernel holds of a state; columns of a workgroup's block of a state; its waves, which take 16
 // columns each.  Rows of wide keys are more than few waves can hold on their way to LDS: these have waves without columns.  So
 // have blocks of five to seven: of workgroups of six waves only one stands on a compute unit at a time, of eight waves two
-// (512 steps of 64 x 32 heads of 96 x 96: 264 us with six waves, 229 with eight, of which two have no columns).
+// (512 steps of 64 x 32 heads of 96 x 96, with numbers in two parts instead of three: 264 us with six waves, 229 with eight, of which
+// two have no columns; now 251).
 inline int la_key_tiles(int Dk) {
     const int t = (Dk + 31) / 32;
     return t <= 4 ? t : t <= 6 ? 6 : 8;
@@ -92,7 +93,8 @@ struct LaPlace {
 
 // The sequence of a rank and its length.  Sequences of a padded batch come longest first, as far as a wave can sort them: the
 // workgroups that start when others have ended are then the short ones.  (57 sequences of 75 to 301 steps, 5 heads of 80 x 160:
-// 31 us, 38 in their order.  Counting the longer ones one by one, not bit by bit, takes 5 us more.)
+// 34 us, 42 in their order.  Counting the longer ones one by one, not bit by bit, takes 5 us more.)  Batches of more than 64
+// sequences, which no wave holds at once, are taken in their order.
 __device__ inline int la_sequence_of_rank(const LaArgs& a, int rank, int* len) {
     if (!a.lengths || a.B > 64) {
         *len = a.lengths ? min(max(a.lengths[rank], 0), a.T) : a.T;

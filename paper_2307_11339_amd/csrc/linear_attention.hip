@@ -194,24 +194,30 @@ __global__ __launch_bounds__(256) void la_join_kernel(const LaArgs a, int64_t pe
     }
 }
 
-// The shortest call that goes in chunks.  A chunk costs the same whether it is full or not: 24 sequences of 8 heads of 128
-// take 11 us in a chunk of up to 64 steps, one step after the other 9.4 (4 steps), 11 (6), 12.8 (8) and 14.3 (10); 64 sequences of 8
-// heads of 64 8.8, and 8.1 (4), 9.1 (6); in fp32 24 of 8 heads of 128 13.6, and 11.6 (6), 13 (8), 15 (10).  One sequence alone takes 8.2
-// us in a chunk, 6.3 (6) and 8.3 (12) one after the other.  4 sequences of 4 heads of 256 take 11.6 us in a chunk, 11 (12 steps) and
-// 12.8 (16) one after the other.
+// The shortest call that goes in chunks: a chunk costs the same whether it is full or not.  The rule is that of many states of up
+// to 128 rows and of few wider ones; it does not look at their number, and what it costs the others is below.  In us, by
+// themselves, a chunk of up to 64 steps and then one step after the other (for so many steps):
+//   64 sequences of 8 heads of 64     8.2     7.0 (4)   8.3 (6)   9.1 (7)   9.9 (8)          fp32  8.6     8.5 (6)   9.4 (7)
+//   24 of 8 heads of 128             10.0     7.7 (4)   9.0 (6)   9.6 (7)  10.3 (8)          fp32 11.6     8.8 (6)  10.3 (8)  12.1 (10)
+//   64 of 16 heads of 128            30.5    28.7 (6)  31.6 (7)  36.0 (8)                    fp32 39.5    32.2 (7)  42.3 (10)
+//   4 of 4 heads of 256              12.1    11.2 (12) 12.2 (14) 13.3 (16)                   fp32 15.7    11.3 (12) 16.6 (20)
+// Few states would be faster one after the other for some steps longer: 1 sequence of 8 heads of 128 8.3, and 5.7 (7), 8.2 (12); of 64
+// 5.9, and 4.7 (7), 6.0 (10).  Of wide ones 16 sequences of 8 heads of 256 would be faster in a chunk from 7 steps on (17.7, and 18.4
+// (7), 25.2 (12)), 64 of them from 14 on (73, and 55 (8), 67 (12), 74 (14)).
 inline int fewest_steps(int Dk) { return Dk > 128 ? 13 : 7; }
 
 // Pieces of long sequences.  Computing the states at the seams costs about 0.4 of the forward itself, so sequences are
 // cut only until every compute unit has eight waves; twice as many pieces, half as long, pay only where a piece still has many
-// steps.  16 heads of 128: 2048 steps of 16 sequences 155 us whole, 190 in two pieces; 65536 steps of one
-// 371 us in 32 pieces, 406 in 16; 4096 steps 49 us in 16 pieces, 57 in 32, 62 in 8; 16 sequences of 512 steps, 8 fp32 heads of
-// 64, all joined by a launch, 42 us in 4 pieces, 46 in 2, 45 in 8.
+// steps.  16 heads of 128: 2048 steps of 16 sequences 178 us whole, 206 in two pieces; 65536 steps of one
+// 408 us in 32 pieces, 465 in 16; 4096 steps 51 us in 16 pieces, 62 in 32, 69 in 8; 16 sequences of 512 steps, 8 fp32 heads of
+// 64, 38 us in 4 pieces, 43 in 2.
 constexpr int LA_WAVES = 2048, LA_LONG_WAVES = 4096;       // eight a compute unit; sixteen
 constexpr int LA_LONG_STEPS = 1024;
 constexpr int LA_PIECE_STEPS = 128;                // of a piece at least
 // Up to so many pieces each adds up by itself what those before it add; more are joined by a launch in between, as the last one
-// would have much to read.  16 sequences of 512 steps, 8 heads of 64: four pieces 24.1 us, joined 26.0 (fp32 39.2 and 41.2); 1024 steps
-// of one, 16 heads of 64: eight pieces 19.1, joined 18.6; 4096 steps, 16 heads of 128: sixteen 55.7, joined 48.7.
+// would have much to read.  16 sequences of 512 steps, 8 heads of 64: four pieces 24.3 us, joined 26.5 (fp32 38.1 and 40.2); 1024 steps
+// of one, 16 heads of 64: eight pieces 18.5, joined 19.0; 4096 steps, 16 heads of 128: sixteen 58.6, joined 50.9; 65536 steps: 32
+// 433, joined 408.
 constexpr int LA_CHAINED_PIECES = 4;
 
 struct LaPlan {

@@ -13,13 +13,15 @@
 // takes its rows in such an order that the two agree: row 4 g + e of result p of the pair is row 8 g + 4 p + e of the 32,
 // and the state goes from accumulator to operand without leaving its lane.
 //
-// What bounds it: the issue of instructions.  A chunk of 128 x 128 takes each of eight waves 97 matrix instructions (of 16
-// cycles) and about 500 vector instructions (of 4 cycles; most of them split numbers) beside 64 KB of memory traffic, and of
-// the two kinds little overlaps: in a loop of their own 520 and 330 cycles, together on one SIMD 757.  2048 steps of 32
-// sequences, 16 heads: 261 us at 2.07 GHz, the clock under this load, the matrix units 37 % of it busy, the vector units 49 %.
-// A copy of as many bytes takes 210, the loads and stores of this kernel without its products 229, the kernel without the extra
-// bf16 numbers 241; four waves of 32 columns with 32 x 32 tiles took 279 between other calls, this 272.  Where one workgroup
-// works by itself on a compute unit (a prompt, a padded batch), a chunk takes 4.2 us, most of it waiting for LDS and at barriers.
+// What a chunk adds to the state is summed up from zero and added to it once, so that a long sequence rounds the state once a chunk.
+//
+// What bounds it: the issue of instructions.  A chunk of 128 x 128 takes each of eight waves 119 matrix instructions (of 16
+// cycles) and 615 vector instructions (of 4 cycles; about 290 of them split numbers) beside 64 KB of memory traffic, and of
+// the two kinds little overlaps: a loop of 520 cycles of the one and a loop of 330 of the other take 757 together on one SIMD.  2048
+// steps of 32 sequences, 16 heads: 318 us at 2.0 GHz, the clock under this load, the matrix units 38 % of it busy, vector instructions
+// without them another 50 %.  A copy of as many bytes takes 210.  With two bf16 numbers for one of fp32 it would take 274, with one
+// 241.  Where one workgroup works by itself on a compute unit (a prompt, a padded batch), most of a chunk is waiting for LDS and at
+// barriers.
 #include <type_traits>
 
 #include "common.h"

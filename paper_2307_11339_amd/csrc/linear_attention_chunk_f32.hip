@@ -3,7 +3,8 @@
 // The formulas and the division of work are those of linear_attention_chunk.hip: each wave owns 16 columns of the state,
 // in its accumulators from the first chunk to the last, and of the outputs; scores pass through LDS.  The products are
 // 16 x 16 x 4 fp32 matrix instructions, a sixteenth of the bf16 rate: the state takes part in two products of 2 Dk Dv a step,
-// which at 128 x 128 take longer than the memory traffic (a third more).  Short chunks have less of the triangle to compute.
+// which at 128 x 128 take longer than the memory traffic (a third more; 2048 steps of 16 sequences, 16 heads: 415 us).  Short chunks
+// have less of the triangle to compute.  What a chunk adds to the state is summed up from zero and added to it once.
 //
 // Operand layouts.  A lane gives one number of an operand, of row (column) l % 16 and index l / 16 of the sum, and any four
 // indices may meet in one instruction.  Where the operand was a result (the state), element e of lane group g is index 4 g + e
