@@ -132,7 +132,7 @@ def _round(x, dtype):
     return torch.from_numpy(x.astype(np.float32)).to(torch.bfloat16 if dtype == BF16 else torch.float32).double().numpy()
 
 
-WIDTHS = sorted({(W, 1) for _, _, W in SHAPES if W >= 64} | {(W, g) for _, _, W, g in GROUPED})
+WIDTHS = sorted({(W, 1) for _, _, W in SHAPES} | {(W, g) for _, _, W, g in GROUPED})
 
 
 def _rows(W, dtype, seed, offset=0.0):
@@ -147,7 +147,7 @@ def _rows(W, dtype, seed, offset=0.0):
 def test_the_bounds_notice_mistakes(W, groups, dtype):
     """A piece of 16 bytes left out of a mean or of the squares, a norm left out: each shows, in either norm, while results that
     are only rounded are far inside."""
-    if (W // groups) % (8 if dtype == BF16 else 4) or W // groups < 32:
+    if (W // groups) % (8 if dtype == BF16 else 4):
         pytest.skip("groups of this width are not taken in this type")
     x, gate, residual, vec = _rows(W, dtype, 1)
     if groups > 1:            # the norm behind the block, by groups
@@ -167,7 +167,7 @@ def test_the_bounds_notice_mistakes(W, groups, dtype):
             assert _worst(_round(bad, dtype), y, ey, dtype) > 1, (mistake, _worst(_round(bad, dtype), y, ey, dtype))
 
 
-@pytest.mark.parametrize("W", sorted({W for _, _, W in SHAPES if W >= 64}))
+@pytest.mark.parametrize("W", sorted({W for _, _, W in SHAPES}))
 def test_the_bounds_notice_a_variance_in_one_pass(W):
     x, _, _, vec = _rows(W, F32, 2, offset=1024.0)
     args = (x, None, None, dict(vec, sc=None), NONE, 1, G_NONE, LAYER, 1e-5, F32)
